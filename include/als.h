@@ -278,6 +278,70 @@ int als_k_attention_bwd(const void* qkv, const void* o, const void* d_o, const f
                         float* dscratch, void* dqkv, int B, int S, int h, int dh, int dtype,
                         int use_mfma, void* stream);
 
+/* ---- a linear layer in 8 bits ---------------------------------------------------------------
+ * A matrix in 8-bit floating point: data [rows, cols] (e4m3: 4 exponent and 3 fraction bits, largest value 448, no
+ * infinity; e5m2: 5 and 2, largest value 57344), rows ld bytes apart, and a scale for each block, one byte s that
+ * stands for 2^(s - 127) and is never 255.  A block is block_rows rows (1 or 128) by 128 columns; those at the edges are smaller.
+ * scale [ceil(rows / block_rows), ceil(cols / 128)], rows ld_scale bytes apart.  An element stands for its 8-bit value times its block's scale.
+ * ld must be a multiple of 16 and at least cols, ld_scale a multiple of 4 and at least ceil(cols / 128); data 16-byte,
+ * scale 4-byte aligned; the last row is ld bytes long like the others, the last scale row ld_scale: what lies behind the columns may be
+ * read and is never used, and never written. */
+#define ALS_FP8_E4M3 0
+#define ALS_FP8_E5M2 1
+typedef struct als_fp8 {
+  void* data;
+  uint8_t* scale;
+  int64_t ld, ld_scale;
+  int32_t format, block_rows;
+} als_fp8;
+
+/* x [rows, cols] (dtype ALS_DTYPE_*, rows ldx elements apart, any alignment) to 8 bits, in one pass over it: q as it is, qt (may be null, q too
+ * if qt is not) transposed, [cols, rows], with blocks of its own along its own rows.  The scale of a block is the least power of two, at least
+ * 2^-127, under which its largest finite magnitude is at most the format's largest value, and 1 for a block without any; every element is divided
+ * by it, which is exact, and rounded to the nearest value, ties to even.  What is not finite is not counted in and shows: NaN becomes NaN, an infinity becomes
+ * NaN in e4m3 and stays one in e5m2.  q and qt may have different formats and block_rows; the three must not overlap. */
+int als_k_quant_fp8(const void* x, int dtype, int rows, int cols, int64_t ldx, const als_fp8* q, const als_fp8* qt, void* stream);
+
+/* Norm of x + resid in one pass, for rows of d <= 16384 elements: total = x + resid; y = total rstd gain (ALS_NORM_RMS; ALS_NORM_LAYER: total
+ * minus its mean), rstd = 1 / sqrt(mean of squares + eps).  x in dtype, resid and total fp32, all [rows, d] without padding; resid and total are both null
+ * (then total is x) or neither; total may be resid, or x in fp32.  y (bf16 [rows, d]) and q (8 bits with block_rows 1, formed from y before its rounding) may
+ * be null, not both.  rstd [rows] is what the backward pass takes. */
+int als_k_norm_fwd(const void* x, int dtype, const float* resid, const float* gain, float* total, void* y, const als_fp8* q, float* rstd,
+                   int rows, int d, double eps, int norm_kind, void* stream);
+/* Its backward pass, with y's gradient dy (dtype) as if y were not rounded: ds = ds_in + rstd (h - xh mean(h xh)), h = dy gain, xh = total rstd
+ * (ALS_NORM_LAYER: total minus its mean, and h minus its own), the gradient of x and of resid alike; dgain [d] = sum over the rows of dy xh, in an order that depends on the
+ * sizes alone.  ds_in (fp32, the gradient that reaches total by other ways) and ds_lp (a bf16 copy of ds) may be null; ds may be ds_in.
+ * ws_dev: 16-byte aligned, at least als_k_norm_bwd_ws_bytes(rows, d) bytes. */
+size_t als_k_norm_bwd_ws_bytes(int rows, int d);
+int als_k_norm_bwd(const void* dy, int dtype, const float* total, const float* rstd, const float* gain, const float* ds_in, float* ds,
+                   void* ds_lp, float* dgain, int rows, int d, int norm_kind, void* ws_dev, size_t ws_bytes, void* stream);
+
+/* C = A.B^T (+ R) of matrices in 8 bits: A [M, K], B [N, K] (the contraction runs along the rows of both, so a weight matrix stored
+ * [K, N] is taken as its transposed form), any two formats and block_rows.  fp32 results: exact products of elements from 2^-126 to 2^127, summed in fp32.  bf16
+ * results: the 8-bit matrix instruction, at up to twice the rate; it sums in fp32 too, but among 8 neighbours in K a product under 2^-13 of the largest may be
+ * lost (1.5e-5 of a sum of random signs; a rounding to bf16 is up to 4e-3).  C [M, N] in out_dtype, rows ldc elements
+ * apart; R (fp32, rows ldr apart) may be null, and may be C itself if that is fp32.  K = 0 gives R or zeros.
+ * ws_dev (256-byte aligned, may be null): scratch for the partial sums of products that are split along K; als_k_gemm_fp8_ws_bytes is what
+ * one takes at most, with less it is split less.  Results do not depend on timing. */
+size_t als_k_gemm_fp8_ws_bytes(int M, int N, int K);
+int als_k_gemm_fp8(const als_fp8* A, const als_fp8* B, void* C, int64_t ldc, int out_dtype, const float* R, int64_t ldr, int M, int N,
+                   int K, void* ws_dev, size_t ws_bytes, void* stream);
+
+/* ---- the global norm of a gradient, and clipping ---------------------------------------------
+ * norm_out[0] = the square root of the sum of the squares of all elements of n tensors (host arrays of device pointers, of element
+ * counts and of ALS_DTYPE_*; dtypes null: all fp32), summed in double in an order that depends on the sizes alone.  Tensors need no alignment beyond their type's;
+ * one without elements may be null.  ws_dev: 16-byte aligned, at least als_k_grad_norm_ws_bytes(n, numel) bytes. */
+size_t als_k_grad_norm_ws_bytes(int n, const int64_t* numel);
+int als_k_grad_norm(int n, const void* const* grads, const int64_t* numel, const int32_t* dtypes, float* norm_out, void* ws_dev,
+                    size_t ws_bytes, void* stream);
+/* The same, and then out_i = grad_i times the coefficient max_norm / norm if norm > max_norm, else 1 (an infinite norm gives 0, a NaN one NaN:
+ * neither is hidden).  out_i in grad_i's type; it may be grad_i, and must not overlap any other tensor: refused. */
+int als_k_grad_clip(int n, const void* const* grads, void* const* outs, const int64_t* numel, const int32_t* dtypes, double max_norm,
+                    float* norm_out, void* ws_dev, size_t ws_bytes, void* stream);
+/* als_k_adamw with the gradient times that coefficient, from a norm on the device: clipping without a pass of its own. */
+int als_k_adamw_clip(float* theta, const float* grad, float* m, float* v, void* bf16_out, int64_t P, int64_t P_decay, int64_t step,
+                     double lr, double beta1, double beta2, double eps, double wd, const float* norm_dev, double max_norm, void* stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -239,6 +239,14 @@ int cast_copy(const float* src, void* dst, int64_t n, int dst_bf16, hipStream_t 
 
 int adamw(float* theta, const float* grad, float* m, float* v, bf16* lp, int64_t P,
           int64_t P_decay, const AdamArgs& a, hipStream_t st, StepState* ss = nullptr);
+// What a gradient of this norm is multiplied with so that it is at most max_norm long.  A norm that is infinite gives 0, NaN gives NaN.
+__device__ __forceinline__ float clip_coefficient(float norm, float max_norm) { return norm <= max_norm ? 1.0f : max_norm / norm; }
+// the same step with the gradient times that coefficient
+struct ClipArgs { const float* norm; float max_norm, rest1, rest2; };   // rest: 1 - beta
+int adamw_clip(float* theta, const float* grad, float* m, float* v, bf16* lp, int64_t P, int64_t P_decay, const AdamArgs& a, const ClipArgs& clip,
+               hipStream_t st, StepState* ss = nullptr);
+// the square root of the sum of the squares of n tensors (grad_norm.hip); partial: scratch of als_k_grad_norm_ws_bytes
+int grad_norm(int n, const void* const* grads, const int64_t* numel, const int32_t* dtypes, float* norm_out, double* partial, hipStream_t st);
 
 #define ALS_DN_MAX_GROUP 16
 struct DnGroup {

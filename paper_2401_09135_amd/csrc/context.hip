@@ -762,6 +762,21 @@ extern "C" int als_k_adamw(float* theta, const float* grad, float* m, float* v, 
   return adamw(theta, grad, m, v, (bf16*)bf16_out, P, P_decay, a, (hipStream_t)stream);
 }
 
+extern "C" int als_k_adamw_clip(float* theta, const float* grad, float* m, float* v, void* bf16_out, int64_t P, int64_t P_decay, int64_t step,
+                                double lr, double beta1, double beta2, double eps, double wd, const float* norm_dev, double max_norm, void* stream) {
+  if (P < 0 || P_decay < 0 || step < 1) return set_error(ALS_ERR_INVALID, "P, P_decay or step out of range");
+  if (!((float)max_norm > 0) || max_norm > 3.4e38) return set_error(ALS_ERR_INVALID, "als_k_adamw_clip: max_norm must be positive and finite");
+  if (P == 0) return ALS_OK;
+  if (!theta || !grad || !m || !v || !norm_dev) return set_error(ALS_ERR_INVALID, "null argument");
+  if (((uintptr_t)theta | (uintptr_t)grad | (uintptr_t)m | (uintptr_t)v) % 16 || (uintptr_t)bf16_out % 8 || (uintptr_t)norm_dev % 4)
+    return set_error(ALS_ERR_INVALID, "als_k_adamw_clip: vectors must be 16-byte aligned, the bf16 copy 8-byte");
+  AdamArgs a;
+  a.lr = (float)lr; a.beta1 = (float)beta1; a.beta2 = (float)beta2; a.eps = (float)eps; a.wd = (float)wd;
+  a.bc1 = (float)(1.0 - pow(beta1, (double)step));
+  a.bc2 = (float)(1.0 - pow(beta2, (double)step));
+  return adamw_clip(theta, grad, m, v, (bf16*)bf16_out, P, P_decay, a, ClipArgs{norm_dev, (float)max_norm, (float)(1.0 - beta1), (float)(1.0 - beta2)}, (hipStream_t)stream);
+}
+
 namespace {
 // the product of the als_k_gemm* entry points: operands without padding
 GemmDesc plain_desc(const void* A, const void* B, void* C, int M, int N, int K, int a_layout, int b_layout, int in_dtype,

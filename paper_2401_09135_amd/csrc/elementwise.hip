@@ -116,6 +116,68 @@ __global__ void adamw_tail_kernel(float* theta, const float* grad, float* m, flo
   if (lp) lp[i] = (bf16)th;
 }
 
+// adam_one with 1 - beta rounded from double: 1 - 0.999f, formed in fp32, is 1.3e-5 below 0.001, and so would v and v's own gradient's share be.
+__device__ __forceinline__ void adam_one_clipped(float& th, float g, float& m, float& v, bool decay, const AdamArgs& a, const ClipArgs& c) {
+  m = a.beta1 * m + c.rest1 * g;
+  v = a.beta2 * v + c.rest2 * g * g;
+  float upd = (m / a.bc1) / (sqrtf(v / a.bc2) + a.eps);
+  if (decay) upd += a.wd * th;
+  th -= a.lr * upd;
+}
+
+// The same with the gradient times the clipping coefficient of its norm, for any P_decay.  Vectors are whole float4 groups; up to three elements behind
+// them are the last threads'.
+template <bool STATE>
+__global__ __launch_bounds__(256) void adamw_clip_kernel(float* __restrict__ theta, const float* __restrict__ grad, float* __restrict__ m,
+                                                         float* __restrict__ v, bf16* __restrict__ lp, int64_t P, int64_t P_decay, AdamArgs a,
+                                                         ClipArgs clip, StepState* ss) {
+  if (STATE) {
+    a = ss->adam;
+    if (blockIdx.x == 0 && threadIdx.x == 0) ss->step++;   // nothing in this kernel reads it
+  }
+  const float k = clip_coefficient(clip.norm[0], clip.max_norm);
+  const int64_t n4 = P / 4, stride = (int64_t)gridDim.x * 256 * STREAM_U;
+  for (int64_t i0 = (int64_t)blockIdx.x * 256 * STREAM_U + threadIdx.x; i0 < n4; i0 += stride) {
+    f32x4 th[STREAM_U], g[STREAM_U], mm[STREAM_U], vv[STREAM_U];
+#pragma unroll
+    for (int u = 0; u < STREAM_U; u++) {
+      int64_t i = i0 + u * 256;
+      if (i < n4) { th[u] = ldnt(theta, i); g[u] = ldnt(grad, i); mm[u] = ldnt(m, i); vv[u] = ldnt(v, i); }
+    }
+#pragma unroll
+    for (int u = 0; u < STREAM_U; u++) {
+      int64_t i = i0 + u * 256;
+      if (i < n4) {
+#pragma unroll
+        for (int e = 0; e < 4; e++) {
+          float t = th[u][e], mo = mm[u][e], ve = vv[u][e];
+          adam_one_clipped(t, g[u][e] * k, mo, ve, 4 * i + e < P_decay, a, clip);
+          th[u][e] = t; mm[u][e] = mo; vv[u][e] = ve;
+        }
+        stnt(theta, i, th[u]); stnt(m, i, mm[u]); stnt(v, i, vv[u]);
+        if (lp) stnt_bf16(lp, i, th[u]);
+      }
+    }
+  }
+  const int64_t i = 4 * n4 + threadIdx.x;
+  if (blockIdx.x == gridDim.x - 1 && i < P) {
+    float th = theta[i], mm = m[i], vv = v[i];
+    adam_one_clipped(th, grad[i] * k, mm, vv, i < P_decay, a, clip);
+    theta[i] = th; m[i] = mm; v[i] = vv;
+    if (lp) lp[i] = (bf16)th;
+  }
+}
+
+int adamw_clip(float* theta, const float* grad, float* m, float* v, bf16* lp, int64_t P, int64_t P_decay, const AdamArgs& a, const ClipArgs& clip,
+               hipStream_t st, StepState* ss) {
+  if (P <= 0) return ALS_OK;
+  const dim3 grid(stream_blocks(P / 4, STREAM_U));
+  if (ss) hipLaunchKernelGGL(adamw_clip_kernel<true>, grid, dim3(256), 0, st, theta, grad, m, v, lp, P, P_decay, a, clip, ss);
+  else hipLaunchKernelGGL(adamw_clip_kernel<false>, grid, dim3(256), 0, st, theta, grad, m, v, lp, P, P_decay, a, clip, ss);
+  ALS_CHECK_LAUNCH();
+  return ALS_OK;
+}
+
 int adamw(float* theta, const float* grad, float* m, float* v, bf16* lp, int64_t P,
           int64_t P_decay, const AdamArgs& a, hipStream_t st, StepState* ss) {
   if (P <= 0) return ALS_OK;
