@@ -2,10 +2,12 @@
 only).  torch supplies device buffers and streams."""
 from __future__ import annotations
 
+import array
 import ctypes as C
 import os
 
 import numpy as np
+import torch
 
 ALS_DTYPE_F32, ALS_DTYPE_BF16 = 0, 1
 VEC = dict(theta=0, momentum=1, delta=2, worker_theta=3, worker_start=4, adam_m=5, adam_v=6, grad=7)
@@ -21,7 +23,6 @@ def _load():
     # libals.so and torch must share ONE HIP runtime in the process (device pointers and
     # streams cross between them): load the runtime torch ships first, so that the
     # library's dependency on libamdhip64 resolves to it by soname.
-    import torch
     rt = os.path.join(os.path.dirname(torch.__file__), "lib", "libamdhip64.so")
     if os.path.exists(rt):
         C.CDLL(rt, mode=C.RTLD_GLOBAL)
@@ -460,16 +461,13 @@ def k_attention_bwd(qkv, o, d_o, lse, dscratch, dqkv, B, S, h, dh, use_mfma=Fals
 
 
 # ---- a linear layer in 8 bits, clipping -----------------------------------------------------------
-FP8_FORMATS = {"e4m3": 0, "e5m2": 1}
-
-
 class _Fp8Struct(C.Structure):
     _fields_ = [("data", _P), ("scale", _P), ("ld", C.c_int64), ("ld_scale", C.c_int64), ("format", C.c_int32),
                 ("block_rows", C.c_int32)]
 
 
 _F8P = C.POINTER(_Fp8Struct)
-lib.als_k_quant_fp8.argtypes = [_P, C.c_int, C.c_int, C.c_int, C.c_int64, _F8P, _F8P, _P]
+lib.als_k_quant_fp8.argtypes = [_P, C.c_int, C.c_int, C.c_int, C.c_int64, _P, _P, _P]
 lib.als_k_norm_fwd.argtypes = [_P, C.c_int, _P, _P, _P, _P, _F8P, _P, C.c_int, C.c_int, C.c_double, C.c_int, _P]
 lib.als_k_norm_bwd_ws_bytes.restype = C.c_size_t
 lib.als_k_norm_bwd_ws_bytes.argtypes = [C.c_int, C.c_int]
@@ -490,25 +488,26 @@ class Fp8:
     column stride, rows a multiple of 16 bytes apart; scale [ceil(rows / block_rows), ceil(cols / 128)] float8_e8m0fnu,
     rows a multiple of 4 bytes apart; block_rows 1 or 128.  Views of wider buffers are taken: see empty()."""
 
-    __slots__ = ("data", "scale", "block_rows", "_c")
+    __slots__ = ("data", "scale", "block_rows", "shape", "device_index", "_c", "_ref")
 
     def __init__(self, data, scale, block_rows: int = 1):
-        import torch
-        fmt = {torch.float8_e4m3fn: 0, torch.float8_e5m2: 1}.get(data.dtype)
+        fmt = _FP8_DTYPES.get(data.dtype)
         if fmt is None or scale.dtype is not torch.float8_e8m0fnu:
             raise AlsError("Fp8: data must be float8_e4m3fn or float8_e5m2, scale float8_e8m0fnu")
-        if block_rows not in (1, 128):
+        if block_rows != 1 and block_rows != 128:
             raise AlsError("Fp8: block_rows must be 1 or 128")
-        if data.dim() != 2 or tuple(scale.shape) != (-(-data.shape[0] // block_rows), -(-data.shape[1] // 128)):
+        self.shape = shape = tuple(data.shape)
+        if len(shape) != 2 or tuple(scale.shape) != (-(-shape[0] // block_rows), -(-shape[1] // 128)):
             raise AlsError("Fp8: scale must be [ceil(rows / block_rows), ceil(cols / 128)] of data [rows, cols]")
-        _check_device("Fp8", data, scale)
-        ld, ld_scale = _row_stride("Fp8: data", data, 16), _row_stride("Fp8: scale", scale, 4)
+        self.device_index = _device("Fp8", data, scale)
         self.data, self.scale, self.block_rows = data, scale, block_rows
-        self._c = _Fp8Struct(data.data_ptr(), scale.data_ptr(), ld, ld_scale, fmt, block_rows)
+        p, ld = _rows_of("Fp8: data", data, 16)
+        ps, ld_scale = _rows_of("Fp8: scale", scale, 4)
+        self._c = _Fp8Struct(p, ps, ld, ld_scale, fmt, block_rows)
+        self._ref = C.byref(self._c)
 
     @classmethod
     def empty(cls, rows: int, cols: int, format: str = "e4m3", block_rows: int = 1, device="cuda:0") -> "Fp8":
-        import torch
         up = lambda n, m: -(-n // m) * m
         dt = {"e4m3": torch.float8_e4m3fn, "e5m2": torch.float8_e5m2}[format]
         kb = -(-cols // 128)
@@ -516,84 +515,102 @@ class Fp8:
         scale = torch.empty(-(-rows // block_rows), up(kb, 4), dtype=torch.uint8, device=device).view(torch.float8_e8m0fnu)[:, :kb]
         return cls(data, scale, block_rows)
 
-    @property
-    def shape(self):
-        return self.data.shape
+
+_FP8_DTYPES = {torch.float8_e4m3fn: 0, torch.float8_e5m2: 1}
+_FLOATS = {torch.float32: ALS_DTYPE_F32, torch.bfloat16: ALS_DTYPE_BF16}
 
 
-def _row_stride(what, t, multiple):
-    """The row stride of a matrix in 8 bits, whose last row has to be as long as the others."""
+def _rows_of(what, t, multiple):
+    """(address, row stride) of a matrix in 8 bits, whose last row has to be as long as the others."""
     rows, cols = t.shape
     if rows == 0 or cols == 0:
-        return -(-cols // multiple) * multiple
-    ld = t.stride(0) if rows > 1 else max(t.stride(0), -(-cols // multiple) * multiple)
-    if (cols > 1 and t.stride(1) != 1) or ld < cols or ld % multiple or t.data_ptr() % multiple:
+        return t.data_ptr(), -(-cols // multiple) * multiple
+    ld, unit = t.stride()
+    if rows == 1:
+        ld = max(ld, -(-cols // multiple) * multiple)
+    p = t.data_ptr()
+    if (unit != 1 and cols > 1) or ld < cols or ld % multiple or p % multiple:
         raise AlsError(f"{what}: columns must be contiguous, the start and the row stride multiples of {multiple} bytes")
     if t.storage_offset() + rows * ld > t.untyped_storage().nbytes():
         raise AlsError(f"{what}: the last row must be as long as the row stride ({ld} bytes)")
-    return ld
+    return p, ld
 
 
-def _check_device(what, *tensors):
-    """All on one GPU (None is skipped); returns the first."""
-    first = None
+def _device(what, *tensors):
+    """The index of the GPU that all of these are on (None is skipped); -1 if there is none."""
+    dev = -1
     for t in tensors:
-        if t is None:
-            continue
-        if not t.is_cuda:
-            raise AlsError(f"{what}: tensors must be on the GPU")
-        if first is None:
-            first = t
-        elif t.device != first.device:
-            raise AlsError(f"{what}: tensors must be on one device")
-    return first
+        if t is not None:
+            d = t.device_index if type(t) is Fp8 else t.get_device()
+            if d < 0:
+                raise AlsError(f"{what}: tensors must be on the GPU")
+            if d != dev:
+                if dev >= 0:
+                    raise AlsError(f"{what}: tensors must be on one device")
+                dev = d
+    return dev
 
 
-def _flat(what, t, dtypes, numel=None):
-    """The address of a contiguous tensor of one of these types; None gives None."""
+def _wrong(what, t, dtypes, numel):
+    raise AlsError(f"{what}: expected a contiguous tensor of {' or '.join(str(d) for d in dtypes)}"
+                   + (f" with {numel} elements" if numel is not None else "") + f", got {tuple(t.shape)} {t.dtype}")
+
+
+def _flat(what, t, dtype, numel):
+    """The address of a contiguous tensor of this type and size; None gives None."""
     if t is None:
         return None
-    if t.dtype not in dtypes or not t.is_contiguous() or (numel is not None and t.numel() != numel):
-        raise AlsError(f"{what}: expected a contiguous tensor of {' or '.join(str(d) for d in dtypes)}"
-                       + (f" with {numel} elements" if numel is not None else "") + f", got {tuple(t.shape)} {t.dtype}")
+    if t.dtype is not dtype or t.numel() != numel or not t.is_contiguous():
+        _wrong(what, t, (dtype,), numel)
     return t.data_ptr()
 
 
-def _call(anchor, fn, *args):
-    """The call with the anchor's GPU as the current one."""
-    import torch
-    if anchor is not None and anchor.device.index != torch.cuda.current_device():
-        with torch.cuda.device(anchor.device):
-            _check(fn(*args))
+def _either(what, t, numel=None):
+    """(address, ALS_DTYPE_*) of a contiguous tensor of fp32 or bf16."""
+    code = _FLOATS.get(t.dtype)
+    if code is None or not t.is_contiguous() or (numel is not None and t.numel() != numel):
+        _wrong(what, t, _FLOATS, numel)
+    return t.data_ptr(), code
+
+
+_gpus = 0
+
+
+def _call(dev, fn, *args):
+    """The call with that GPU as the current one."""
+    global _gpus
+    _gpus = _gpus or torch.cuda.device_count()
+    if _gpus > 1 and dev >= 0 and dev != torch.cuda.current_device():
+        with torch.cuda.device(dev):
+            rc = fn(*args)
     else:
-        _check(fn(*args))
+        rc = fn(*args)
+    if rc:
+        _check(rc)
 
 
-def _ws(what, ws, need, align):
+def _ws(what, ws):
     if ws is None:
-        if need:
-            raise AlsError(f"{what}: needs a workspace of {need} bytes")
         return None, 0
     if not ws.is_contiguous():
         raise AlsError(f"{what}: the workspace must be contiguous")
     return ws.data_ptr(), ws.numel() * ws.element_size()
 
 
-def _float_types():
-    import torch
-    return torch.float32, torch.bfloat16
-
-
 def k_quant_fp8(x, q=None, qt=None, stream=None):
     """als_k_quant_fp8: x [rows, cols] fp32 or bf16 (unit column stride) to 8 bits, q [rows, cols] and / or qt [cols, rows] (Fp8)."""
-    if x.dtype not in _float_types() or x.dim() != 2 or (x.shape[1] > 1 and x.stride(1) != 1) or (x.shape[0] > 1 and x.stride(0) < x.shape[1]):
+    code = _FLOATS.get(x.dtype)
+    if code is None or x.dim() != 2:
         raise AlsError("k_quant_fp8: x must be a matrix of fp32 or bf16 with unit column stride")
-    rows, cols = x.shape
-    if (q is not None and tuple(q.shape) != (rows, cols)) or (qt is not None and tuple(qt.shape) != (cols, rows)):
+    (rows, cols), (ldx, unit) = x.shape, x.stride()
+    if rows <= 1:
+        ldx = cols
+    if (cols > 1 and unit != 1) or ldx < cols:
+        raise AlsError("k_quant_fp8: x must be a matrix of fp32 or bf16 with unit column stride")
+    if (q is not None and q.shape != (rows, cols)) or (qt is not None and qt.shape != (cols, rows)):
         raise AlsError("k_quant_fp8: q must be [rows, cols] and qt [cols, rows]")
-    _check_device("k_quant_fp8", x, q and q.data, qt and qt.data)
-    _call(x, lib.als_k_quant_fp8, x.data_ptr(), _dt(x), rows, cols, x.stride(0) if rows > 1 else cols, C.byref(q._c) if q else None,
-          C.byref(qt._c) if qt else None, _stream_handle(stream))
+    _call(_device("k_quant_fp8", x, q, qt), lib.als_k_quant_fp8, x.data_ptr(), code, rows, cols, ldx, q._ref if q is not None else None,
+          qt._ref if qt is not None else None, _stream_handle(stream))
 
 
 NORM_KINDS = {"rms": 0, "layer": 1}
@@ -601,16 +618,15 @@ NORM_KINDS = {"rms": 0, "layer": 1}
 
 def k_norm_fwd(x, gain, resid=None, total=None, y=None, q=None, rstd=None, norm="rms", eps=1e-5, stream=None):
     """als_k_norm_fwd: total = x + resid and its norm, in bf16 (y) and / or 8 bits (q, Fp8); x [rows, d] fp32 or bf16."""
-    import torch
+    what, f32 = "k_norm_fwd", torch.float32
     rows, d = x.shape
-    f32, n = (torch.float32,), rows * d
-    if q is not None and tuple(q.shape) != (rows, d):
+    n = rows * d
+    if q is not None and q.shape != (rows, d):
         raise AlsError("k_norm_fwd: q must be [rows, d]")
-    _check_device("k_norm_fwd", x, gain, resid, total, y, q and q.data, rstd)
-    what = "k_norm_fwd"
-    _call(x, lib.als_k_norm_fwd, _flat(what, x, _float_types()), _dt(x), _flat(what, resid, f32, n), _flat(what, gain, f32, d), _flat(what, total, f32, n),
-          _flat(what, y, (torch.bfloat16,), n), C.byref(q._c) if q else None, _flat(what, rstd, f32, rows), rows, d, float(eps), NORM_KINDS[norm],
-          _stream_handle(stream))
+    dev = _device(what, x, gain, resid, total, y, q, rstd)
+    px, code = _either(what, x)
+    _call(dev, lib.als_k_norm_fwd, px, code, _flat(what, resid, f32, n), _flat(what, gain, f32, d), _flat(what, total, f32, n),
+          _flat(what, y, torch.bfloat16, n), q._ref if q is not None else None, _flat(what, rstd, f32, rows), rows, d, eps, NORM_KINDS[norm], _stream_handle(stream))
 
 
 def k_norm_bwd_ws_bytes(rows: int, d: int) -> int:
@@ -619,14 +635,13 @@ def k_norm_bwd_ws_bytes(rows: int, d: int) -> int:
 
 def k_norm_bwd(dy, total, rstd, gain, ds, dgain, ws, ds_in=None, ds_lp=None, norm="rms", stream=None):
     """als_k_norm_bwd: ds (and its bf16 copy ds_lp) and dgain from dy [rows, d] (fp32 or bf16) and what k_norm_fwd left."""
-    import torch
+    what, f32 = "k_norm_bwd", torch.float32
     rows, d = dy.shape
-    f32, n = (torch.float32,), rows * d
-    what = "k_norm_bwd"
-    _check_device(what, dy, total, rstd, gain, ds, dgain, ws, ds_in, ds_lp)
-    _call(dy, lib.als_k_norm_bwd, _flat(what, dy, _float_types()), _dt(dy), _flat(what, total, f32, n), _flat(what, rstd, f32, rows),
-          _flat(what, gain, f32, d), _flat(what, ds_in, f32, n), _flat(what, ds, f32, n), _flat(what, ds_lp, (torch.bfloat16,), n),
-          _flat(what, dgain, f32, d), rows, d, NORM_KINDS[norm], *_ws(what, ws, k_norm_bwd_ws_bytes(rows, d), 16), _stream_handle(stream))
+    n = rows * d
+    dev = _device(what, dy, total, rstd, gain, ds, dgain, ws, ds_in, ds_lp)
+    p, code = _either(what, dy)
+    _call(dev, lib.als_k_norm_bwd, p, code, _flat(what, total, f32, n), _flat(what, rstd, f32, rows), _flat(what, gain, f32, d), _flat(what, ds_in, f32, n),
+          _flat(what, ds, f32, n), _flat(what, ds_lp, torch.bfloat16, n), _flat(what, dgain, f32, d), rows, d, NORM_KINDS[norm], *_ws(what, ws), _stream_handle(stream))
 
 
 def k_gemm_fp8_ws_bytes(M: int, N: int, K: int) -> int:
@@ -635,28 +650,65 @@ def k_gemm_fp8_ws_bytes(M: int, N: int, K: int) -> int:
 
 def k_gemm_fp8(a, b, c, resid=None, ws=None, stream=None):
     """als_k_gemm_fp8: c [M, N] (fp32 or bf16) = a b^T (+ resid, fp32), a [M, K] and b [N, K] Fp8; ws: uint8 of k_gemm_fp8_ws_bytes."""
-    (M, K), N = a.shape, b.shape[0]
     what = "k_gemm_fp8"
-    if b.shape[1] != K or tuple(c.shape) != (M, N) or (resid is not None and tuple(resid.shape) != (M, N)):
-        raise AlsError("k_gemm_fp8: a [M, K], b [N, K], c and resid [M, N]")
-    import torch
-    for t, types in ((c, _float_types()), (resid, (torch.float32,))):
-        if t is not None and (t.dtype not in types or (N > 1 and t.stride(1) != 1) or (M > 1 and t.stride(0) < N)):
-            raise AlsError("k_gemm_fp8: c (fp32 or bf16) and resid (fp32) must have unit column stride")
-    _check_device(what, a.data, b.data, c, resid, ws)
-    _call(c, lib.als_k_gemm_fp8, C.byref(a._c), C.byref(b._c), c.data_ptr(), c.stride(0) if M > 1 else N, _dt(c),
-          resid.data_ptr() if resid is not None else None, (resid.stride(0) if M > 1 else N) if resid is not None else 0, M, N, K, *_ws(what, ws, 0, 256),
-          _stream_handle(stream))
+    M, K = a.shape
+    N, kb = b.shape
+    code = _FLOATS.get(c.dtype)
+    if kb != K or c.shape != (M, N) or code is None:
+        raise AlsError("k_gemm_fp8: a [M, K], b [N, K], c and resid [M, N], c in fp32 or bf16, resid in fp32")
+    ldc, unit = c.stride()
+    if M <= 1:
+        ldc = N
+    pr = ldr = 0
+    if resid is not None:
+        if resid.shape != (M, N) or resid.dtype is not torch.float32:
+            raise AlsError("k_gemm_fp8: a [M, K], b [N, K], c and resid [M, N], c in fp32 or bf16, resid in fp32")
+        pr = resid.data_ptr()
+        ldr, unit_r = resid.stride()
+        if M <= 1:
+            ldr = N
+        if N > 1 and unit_r != 1:
+            unit = unit_r
+    if (N > 1 and unit != 1) or ldc < N or (pr and ldr < N):
+        raise AlsError("k_gemm_fp8: c and resid must have unit column stride")
+    _call(_device(what, a, b, c, resid, ws), lib.als_k_gemm_fp8, a._ref, b._ref, c.data_ptr(), ldc, code, pr or None, ldr, M, N, K, *_ws(what, ws), _stream_handle(stream))
 
 
-def _grad_list(what, tensors):
-    import torch
-    n = len(tensors)
+lib.als_k_set_gemm_fp8.argtypes = [C.c_int, C.c_int]
+lib.als_k_gemm_fp8_route.argtypes = [C.c_int, C.c_int, C.c_int, C.c_int, C.c_size_t, C.POINTER(C.c_int), C.POINTER(C.c_int)]
+
+
+def set_gemm_fp8(tile: int, shares: int = 1) -> None:
+    """Tuning hook: force the tile (256, 128, 64; 0 = automatic) and the shares of K of k_gemm_fp8."""
+    _check(lib.als_k_set_gemm_fp8(tile, shares if tile else 0))
+
+
+def gemm_fp8_route(M, N, K, out_dtype=ALS_DTYPE_BF16, ws_bytes=None):
+    """(tile, shares of K) that k_gemm_fp8 takes for a product (host only); ws_bytes None: as much as it asks for."""
+    tile, shares = C.c_int(), C.c_int()
+    _check(lib.als_k_gemm_fp8_route(M, N, K, out_dtype, k_gemm_fp8_ws_bytes(M, N, K) if ws_bytes is None else ws_bytes, C.byref(tile), C.byref(shares)))
+    return tile.value, shares.value
+
+
+def _addresses(values):
+    """A host array of 64-bit values and its address."""
+    a = array.array("q", values)
+    return a, a.buffer_info()[0]
+
+
+def _grad_list(what, tensors, dev):
+    """Host arrays of the addresses, element counts and types of contiguous tensors of fp32 or bf16 on the GPU dev."""
+    p, numel, dtypes = [], [], []
     for t in tensors:
-        _flat(what, t, _float_types())
-    numel = (C.c_int64 * n)(*[t.numel() for t in tensors])
-    dtypes = (C.c_int32 * n)(*[1 if t.dtype is torch.bfloat16 else 0 for t in tensors])
-    return n, numel, dtypes
+        code = _FLOATS.get(t.dtype)
+        if code is None or not t.is_contiguous():
+            _wrong(what, t, _FLOATS, None)
+        if t.get_device() != dev:
+            raise AlsError(f"{what}: tensors must be on the GPU, and on one")
+        p.append(t.data_ptr())
+        numel.append(t.numel())
+        dtypes.append(code)
+    return p, numel, dtypes
 
 
 def k_grad_norm_ws_bytes(grads) -> int:
@@ -666,30 +718,29 @@ def k_grad_norm_ws_bytes(grads) -> int:
 
 def k_grad_norm(grads, norm, ws, stream=None):
     """als_k_grad_norm: norm[0] (fp32, on the GPU) = the 2-norm of all elements of a list of contiguous fp32 / bf16 tensors."""
-    import torch
     what = "k_grad_norm"
-    n, numel, dtypes = _grad_list(what, grads)
-    _check_device(what, norm, ws, *grads)
-    _call(norm, lib.als_k_grad_norm, n, _ptr_array(grads), numel, dtypes, _flat(what, norm, (torch.float32,), 1), *_ws(what, ws, 0, 16), _stream_handle(stream))
+    dev = _device(what, norm, ws)
+    p, numel, dtypes = _grad_list(what, grads, dev)
+    (ap, p), (an, numel_p), at = _addresses(p), _addresses(numel), array.array("i", dtypes)
+    _call(dev, lib.als_k_grad_norm, len(grads), p, numel_p, at.buffer_info()[0], _flat(what, norm, torch.float32, 1), *_ws(what, ws), _stream_handle(stream))
 
 
 def k_grad_clip(grads, outs, max_norm, norm, ws, stream=None):
     """als_k_grad_clip: the same, and outs[i] = grads[i] scaled so that the norm is at most max_norm; outs may be grads."""
-    import torch
     what = "k_grad_clip"
-    n, numel, dtypes = _grad_list(what, grads)
-    if len(outs) != n or any(o.numel() != g.numel() or o.dtype != g.dtype or not o.is_contiguous() for o, g in zip(outs, grads)):
-        raise AlsError("k_grad_clip: outs must match grads in number, sizes and types, and be contiguous")
-    _check_device(what, norm, ws, *grads, *outs)
-    _call(norm, lib.als_k_grad_clip, n, _ptr_array(grads), _ptr_array(outs), numel, dtypes, float(max_norm), _flat(what, norm, (torch.float32,), 1),
-          *_ws(what, ws, 0, 16), _stream_handle(stream))
+    dev = _device(what, norm, ws)
+    p, numel, dtypes = _grad_list(what, grads, dev)
+    po, numel_o, dtypes_o = (p, numel, dtypes) if outs is grads else _grad_list(what, outs, dev)
+    if numel_o != numel or dtypes_o != dtypes:
+        raise AlsError("k_grad_clip: outs must match grads in number, sizes and types")
+    (ap, p), (ao, po), (an, numel_p), at = _addresses(p), _addresses(po), _addresses(numel), array.array("i", dtypes)
+    _call(dev, lib.als_k_grad_clip, len(grads), p, po, numel_p, at.buffer_info()[0], float(max_norm), _flat(what, norm, torch.float32, 1), *_ws(what, ws),
+          _stream_handle(stream))
 
 
 def k_adamw_clip(theta, grad, m, v, bf16_out, P_decay, step, lr, norm, max_norm, beta1=0.9, beta2=0.999, eps=1e-8, wd=0.1, stream=None):
     """k_adamw with the gradient scaled so that its norm (norm[0], on the GPU: k_grad_norm) is at most max_norm."""
-    import torch
-    what, f32, P = "k_adamw_clip", (torch.float32,), theta.numel()
-    _check_device(what, theta, grad, m, v, bf16_out, norm)
-    _call(theta, lib.als_k_adamw_clip, _flat(what, theta, f32), _flat(what, grad, f32, P), _flat(what, m, f32, P), _flat(what, v, f32, P),
-          _flat(what, bf16_out, (torch.bfloat16,), P), P, int(P_decay), int(step), float(lr), float(beta1), float(beta2), float(eps), float(wd),
-          _flat(what, norm, f32, 1), float(max_norm), _stream_handle(stream))
+    what, f32, P = "k_adamw_clip", torch.float32, theta.numel()
+    dev = _device(what, theta, grad, m, v, bf16_out, norm)
+    _call(dev, lib.als_k_adamw_clip, _flat(what, theta, f32, P), _flat(what, grad, f32, P), _flat(what, m, f32, P), _flat(what, v, f32, P),
+          _flat(what, bf16_out, torch.bfloat16, P), P, P_decay, step, lr, beta1, beta2, eps, wd, _flat(what, norm, f32, 1), max_norm, _stream_handle(stream))

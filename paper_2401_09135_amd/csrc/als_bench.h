@@ -43,6 +43,11 @@ int als_k_gemm_dw_grouped_plan(int n, const int* M, const int* N, int K, int max
  * borders of the dispatch.  Arguments as als_k_gemm_ex, operands taken as 256-byte aligned; flags as als_config.flags. */
 int als_k_gemm_route(int M, int N, int K, int a_layout, int b_layout, int in_dtype, int out_dtype, int epi, int flags,
                      size_t ws_bytes, char* out, int out_len);
+/* Test and tuning hook: make als_k_gemm_fp8 take tiles of 256, 128 or 64 and that many shares of K (as many as there are slices and the workspace holds, else 1);
+ * tile 0: the choice by size again.  Process-wide. */
+int als_k_set_gemm_fp8(int tile, int shares);
+/* Host only: the tile and the shares of K that als_k_gemm_fp8 takes for a product with a workspace of ws_bytes. */
+int als_k_gemm_fp8_route(int M, int N, int K, int out_dtype, size_t ws_bytes, int* tile_out, int* shares_out);
 /* Host only: the kernel that orders a call's tokens by id (n_steps steps of T positions, vocabulary V). */
 int als_k_token_order_route(int T, int V, int n_steps, char* out, int out_len);
 /* Host only: how the embedding gradient of a step of T positions is formed (vocabulary V, width d). */

@@ -76,7 +76,10 @@ __global__ __launch_bounds__(NT == 64 ? 256 : NT) void norm_fwd_kernel(NormFwdAr
 #pragma unroll
     for (int i = 0; i < 8; i++) ss += v[s][i] * v[s][i];
   ss = row_sum<NT>(ss, sh);
-  const float r = 1.0f / sqrtf(ss / (float)a.d + a.eps);
+  // rstd in two parts, and each product with what its rounding left: an output in 8 bits turns an error of one rounding into a step of 1/16 where it falls on a border,
+  // and what follows is rounded once.  (In the shadow of memory: 0.2 us of 45.)
+  const double rd = 1.0 / sqrt((double)ss / a.d + (double)a.eps);
+  const float r = (float)rd, r_rest = (float)(rd - (double)r);
   if (t == 0) a.rstd[row] = r;
 #pragma unroll
   for (int s = 0; s < NORM_RUNS; s++) {
@@ -84,7 +87,10 @@ __global__ __launch_bounds__(NT == 64 ? 256 : NT) void norm_fwd_kernel(NormFwdAr
     float g[8];
     load8<VEC>(a.gain + c, n, g);
 #pragma unroll
-    for (int i = 0; i < 8; i++) v[s][i] = v[s][i] * r * g[i];
+    for (int i = 0; i < 8; i++) {
+      const float p = v[s][i] * g[i], p_rest = fmaf(v[s][i], g[i], -p);
+      v[s][i] = fmaf(p, r, fmaf(p, r_rest, p_rest * r));
+    }
     if (a.y) store8<VEC>(a.y + base + c, n, v[s]);
     if (a.q) {
       float m = 0.0f;

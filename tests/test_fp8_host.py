@@ -143,3 +143,37 @@ def test_binding_refuses_tensors_of_the_host_and_of_other_types():
         A.k_quant_fp8(x.t())
     with pytest.raises(A.AlsError, match="GPU"):
         A.k_grad_norm([x], x[0, :1], x)
+
+
+def test_product_kernels_by_size():
+    """The choices that the rule's comment gives figures for, and what it asks for as a workspace."""
+    for (M, N, K), want in {(896, 3584, 15315): (128, 1), (1024, 896, 3584): (64, 1), (2048, 2048, 2048): (128, 1), (16384, 3584, 896): (256, 1), (16384, 896, 896): (256, 1),
+                            (5, 3584, 896): (64, 1), (1, 1, 1): (64, 1), (8192, 8192, 8192): (256, 1)}.items():
+        assert A.gemm_fp8_route(M, N, K) == want, (M, N, K)
+        # without a workspace nothing is split, whatever the size
+        assert A.gemm_fp8_route(M, N, K, ws_bytes=0)[1] == 1
+    assert A.gemm_fp8_route(896, 3584, 15315, 0) == (256, 4)
+    tile, shares = A.gemm_fp8_route(1, 8192, 8192)
+    assert tile == 64 and shares > 1
+    rng = __import__("random").Random(0)
+    for _ in range(300):
+        M, N, K = (int(2 ** rng.uniform(0, b)) for b in (17, 15, 17))
+        need = A.k_gemm_fp8_ws_bytes(M, N, K)
+        for dt in (0, 1):
+            tile, shares = A.gemm_fp8_route(M, N, K, dt)
+            slices = -(-K // 128)
+            assert tile in (64, 128, 256) and 1 <= shares <= max(1, slices // 2) and (shares == 1 or shares * M * (-(-N // 4) * 4) * 4 <= need <= 256 << 20)
+            some = need // 2
+            t2, s2 = A.gemm_fp8_route(M, N, K, dt, ws_bytes=some)
+            assert s2 == 1 or s2 * M * (-(-N // 4) * 4) * 4 <= some
+    assert A.k_gemm_fp8_ws_bytes(0, 5, 5) == 0 and A.k_gemm_fp8_ws_bytes(5, 5, 0) == 0
+
+
+@pytest.mark.parametrize("tile,shares", [(32, 1), (256, 0), (64, 65), (0, -1)])
+def test_product_hook_refuses(tile, shares):
+    assert lib.als_k_set_gemm_fp8(tile, shares) == INVALID
+
+
+@pytest.mark.parametrize("bad", [dict(ldc=(1 << 26) + 1), dict(r=P16 + 64, ldr=(1 << 26) + 1), dict(N=(1 << 20) + 1, ldc=1 << 21), dict(a=dict(ld=(1 << 23) + 16)), dict(b=dict(ld_scale=(1 << 23) + 4))])
+def test_gemm_refuses_what_its_addresses_do_not_reach(bad):
+    assert gemm(**bad) == INVALID

@@ -279,6 +279,63 @@ def test_product_of_whole_numbers_is_exact(M, N, K, fa, fb, ra, rb, with_ws):
     assert torch.equal(rc.cpu().double(), want + r.double())
 
 
+VARIANT_SIZES = [(1, 1, 1), (65, 63, 130), (100, 257, 15), (257, 511, 385), (513, 100, 2049), (300, 1000, 48), (31, 2000, 4097), (1500, 40, 3000), (640, 896, 640), (1100, 2100, 1500)]
+
+
+@pytest.mark.parametrize("tile", [256, 128, 64])
+@pytest.mark.parametrize("shares", [1, 2, 3, 5])
+def test_every_kernel_takes_every_size(tile, shares):
+    try:
+        for i, (M, N, K) in enumerate(VARIANT_SIZES):
+            fa, fb, ra, rb = [("e4m3", "e4m3", 1, 128), ("e5m2", "e4m3", 1, 1), ("e4m3", "e5m2", 128, 1)][(i + shares) % 3]
+            a, b = int_operand(M, K, fa, ra, 1, 4), int_operand(N, K, fb, rb, 2, 4)
+            want = wide(a) @ wide(b).t()
+            r = torch.randint(-100, 100, (M, N), generator=torch.Generator().manual_seed(3)).float() / 4
+            A.set_gemm_fp8(tile, shares)
+            ws = torch.full((shares * M * (N + 3) * 4 + 256,), 0xFF, dtype=torch.uint8, device=DEV)
+            # aligned rows, and rows at odd addresses, inside a larger matrix; with and without something added
+            for pad in (-N % 16 + 16, 1):
+                for dt in (torch.float32, torch.bfloat16):
+                    for add in (None, r):
+                        big = torch.full((M + 2, N + pad), 7.0, dtype=dt, device=DEV)
+                        c = big[1:M + 1, :N]
+                        A.k_gemm_fp8(a, b, c, resid=add.to(DEV) if add is not None else None, ws=ws)
+                        assert torch.equal(c.cpu(), (want + (add.double() if add is not None else 0)).float().to(dt)), (M, N, K, pad, dt, add is None)
+                        big[1:M + 1, :N] = 7.0
+                        assert (big == 7.0).all()
+    finally:
+        A.set_gemm_fp8(0)
+
+
+def test_a_small_workspace_means_fewer_shares():
+    M, N, K = 64, 512, 8192
+    tile, shares = A.gemm_fp8_route(M, N, K)
+    assert shares > 1 and A.gemm_fp8_route(M, N, K, ws_bytes=0)[1] == 1
+    a, b = int_operand(M, K, "e4m3", 1, 1, 4), int_operand(N, K, "e4m3", 128, 2, 4)
+    want = wide(a) @ wide(b).t()
+    c = torch.empty(M, N, device=DEV)
+    for size in (0, 256, M * N * 4 * 2, A.k_gemm_fp8_ws_bytes(M, N, K)):
+        ws = torch.full((size + 512,), 0x55, dtype=torch.uint8, device=DEV)
+        c.zero_()
+        A.k_gemm_fp8(a, b, c, ws=ws[:size] if size else None)
+        assert torch.equal(c.cpu().double(), want) and (ws[size:] == 0x55).all()
+
+
+@pytest.mark.parametrize("M,N,K", [(70, 80, 300), (300, 257, 300)])
+def test_product_with_the_least_scale(M, N, K):
+    """2^-127, which is no normal fp32 number: the elements of A are 2^-125 to 2^-124 there."""
+    a, b = int_operand(M, K, "e4m3", 1, 5, 4), int_operand(N, K, "e4m3", 1, 6, 4)
+    a.data.copy_((4 + 4 * (torch.arange(K) % 2)).float().to(DT["e4m3"]).to(DEV).expand(M, K))
+    a.scale.view(torch.uint8).fill_(0)
+    b.scale.view(torch.uint8).fill_(127 + 100)
+    want = wide(a) @ wide(b).t()
+    c, h = torch.empty(M, N, device=DEV), torch.empty(M, N, dtype=torch.bfloat16, device=DEV)
+    A.k_gemm_fp8(a, b, c)
+    assert torch.equal(c.cpu().double(), want)
+    A.k_gemm_fp8(a, b, h)
+    assert torch.equal(h.cpu(), want.float().bfloat16())
+
+
 @pytest.mark.parametrize("M,N,K", [(200, 300, 1000), (256, 512, 4096), (3, 700, 15315), (1000, 900, 129)])
 @pytest.mark.parametrize("fa,fb", [("e4m3", "e4m3"), ("e5m2", "e4m3")])
 def test_product_of_quantised_values(M, N, K, fa, fb):
