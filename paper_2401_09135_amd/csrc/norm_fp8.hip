@@ -38,30 +38,34 @@ struct NormFwdArgs {
 };
 
 // NT threads a row; NT = 64: four rows a workgroup
-template <typename T, int NT, bool VEC, bool CENTER>
+template <typename T, int NT, bool CENTER>
 __global__ __launch_bounds__(NT == 64 ? 256 : NT) void norm_fwd_kernel(NormFwdArgs a) {
   __shared__ float sh[NT / 64];
   const int t = NT == 64 ? threadIdx.x & 63 : threadIdx.x;
   const int row = NT == 64 ? blockIdx.x * 4 + (threadIdx.x >> 6) : blockIdx.x;
   if (row >= a.rows) return;   // a whole wavefront, or nobody where the threads of a row meet
   const int64_t base = (int64_t)row * a.d;
-  float v[NORM_RUNS][8];
+  float v[NORM_RUNS][8], e[NORM_RUNS][8];
   float sum = 0.0f;
 #pragma unroll
-  for (int s = 0; s < NORM_RUNS; s++) {
-    const int c = 8 * (t + NT * s), n = a.d - c;
-    load8<VEC>((const T*)a.x + base + c, n, v[s]);
-    if (a.resid) {
-      float r[8];
-      load8<VEC>(a.resid + base + c, n, r);
+  for (int s = 0; s < NORM_RUNS; s++) load8((const T*)a.x + base + 8 * (t + NT * s), a.d - 8 * (t + NT * s), v[s]);
+  if (a.resid) {
 #pragma unroll
-      for (int i = 0; i < 8; i++) v[s][i] += r[i];
-      store8<VEC>(a.total + base + c, n, v[s]);
+    for (int s = 0; s < NORM_RUNS; s++) load8(a.resid + base + 8 * (t + NT * s), a.d - 8 * (t + NT * s), e[s]);
+#pragma unroll
+    for (int s = 0; s < NORM_RUNS; s++) {
+#pragma unroll
+      for (int i = 0; i < 8; i++) v[s][i] += e[s][i];
+      store8(a.total + base + 8 * (t + NT * s), a.d - 8 * (t + NT * s), v[s]);
     }
-    if (CENTER)
+  }
+#pragma unroll
+  for (int s = 0; s < NORM_RUNS; s++) load8(a.gain + 8 * (t + NT * s), a.d - 8 * (t + NT * s), e[s]);
+  if (CENTER)
+#pragma unroll
+    for (int s = 0; s < NORM_RUNS; s++)
 #pragma unroll
       for (int i = 0; i < 8; i++) sum += v[s][i];
-  }
   if (CENTER) {
     const float mean = row_sum<NT>(sum, sh) / (float)a.d;
 #pragma unroll
@@ -77,33 +81,29 @@ __global__ __launch_bounds__(NT == 64 ? 256 : NT) void norm_fwd_kernel(NormFwdAr
     for (int i = 0; i < 8; i++) ss += v[s][i] * v[s][i];
   ss = row_sum<NT>(ss, sh);
   // rstd in two parts, and each product with what its rounding left: an output in 8 bits turns an error of one rounding into a step of 1/16 where it falls on a border,
-  // and what follows is rounded once.  (In the shadow of memory: 0.2 us of 45.)
+  // and what follows is rounded once.  (0.5 us of 48.)
   const double rd = 1.0 / sqrt((double)ss / a.d + (double)a.eps);
   const float r = (float)rd, r_rest = (float)(rd - (double)r);
   if (t == 0) a.rstd[row] = r;
 #pragma unroll
   for (int s = 0; s < NORM_RUNS; s++) {
     const int c = 8 * (t + NT * s), n = a.d - c;
-    float g[8];
-    load8<VEC>(a.gain + c, n, g);
 #pragma unroll
     for (int i = 0; i < 8; i++) {
-      const float p = v[s][i] * g[i], p_rest = fmaf(v[s][i], g[i], -p);
+      const float p = v[s][i] * e[s][i], p_rest = fmaf(v[s][i], e[s][i], -p);
       v[s][i] = fmaf(p, r, fmaf(p, r_rest, p_rest * r));
     }
-    if (a.y) store8<VEC>(a.y + base + c, n, v[s]);
+    if (a.y) store8(a.y + base + c, n, v[s]);
     if (a.q) {
-      float m = 0.0f;
+      unsigned m = 0;
 #pragma unroll
-      for (int i = 0; i < 8; i++) m = fmaxf(m, fp8_magnitude(v[s][i]));
-#pragma unroll
-      for (int o = 1; o < 16; o <<= 1) m = fmaxf(m, __shfl_xor(m, o, 64));
-      const int b = fp8_scale_byte(m, a.format);
-      const float iv = fp8_inv_scale(b);
+      for (int i = 0; i < 8; i++) m = max(m, fp8_magnitude(v[s][i]));
+      const int b = fp8_scale_byte(lanes16_max(m), a.format);
+      const float sc = fp8_scale(b);
       if (n > 0) {
         if ((t & 15) == 0) a.scale[(int64_t)row * a.ld_scale + c / 128] = (uint8_t)b;
-        store8_bytes(a.q + (int64_t)row * a.ld + c, n, fp8_pack4(v[s][0] * iv, v[s][1] * iv, v[s][2] * iv, v[s][3] * iv, a.format),
-                     fp8_pack4(v[s][4] * iv, v[s][5] * iv, v[s][6] * iv, v[s][7] * iv, a.format));
+        store8_bytes(a.q + (int64_t)row * a.ld + c, n, fp8_pack4(v[s][0], v[s][1], v[s][2], v[s][3], sc, a.format),
+                     fp8_pack4(v[s][4], v[s][5], v[s][6], v[s][7], sc, a.format));
       }
     }
   }
@@ -121,7 +121,7 @@ int norm_bwd_blocks(int rows, int d) {
   return b < 512 ? b : 512;
 }
 
-template <typename T, int NT, bool VEC, bool CENTER>
+template <typename T, int NT, bool CENTER>
 __global__ __launch_bounds__(NT == 64 ? 256 : NT) void norm_bwd_kernel(NormBwdArgs a) {
   constexpr int AT_ONCE = NT == 64 ? 4 : 1;
   __shared__ float sh[NT / 64];
@@ -131,7 +131,7 @@ __global__ __launch_bounds__(NT == 64 ? 256 : NT) void norm_bwd_kernel(NormBwdAr
   float dg[NORM_RUNS][8], g[NORM_RUNS][8];
 #pragma unroll
   for (int s = 0; s < NORM_RUNS; s++) {
-    load8<VEC>(a.gain + 8 * (t + NT * s), a.d - 8 * (t + NT * s), g[s]);
+    load8(a.gain + 8 * (t + NT * s), a.d - 8 * (t + NT * s), g[s]);
 #pragma unroll
     for (int i = 0; i < 8; i++) dg[s][i] = 0.0f;
   }
@@ -143,8 +143,8 @@ __global__ __launch_bounds__(NT == 64 ? 256 : NT) void norm_bwd_kernel(NormBwdAr
 #pragma unroll
     for (int s = 0; s < NORM_RUNS; s++) {
       const int c = 8 * (t + NT * s), n = a.d - c;
-      load8<VEC>(a.total + base + c, n, x[s]);
-      load8<VEC>((const T*)a.dy + base + c, n, h[s]);
+      load8(a.total + base + c, n, x[s]);
+      load8((const T*)a.dy + base + c, n, h[s]);
       if (CENTER)
 #pragma unroll
         for (int i = 0; i < 8; i++) sx += x[s][i];
@@ -171,19 +171,19 @@ __global__ __launch_bounds__(NT == 64 ? 256 : NT) void norm_bwd_kernel(NormBwdAr
       for (int i = 0; i < 8; i++) o[i] = r * (h[s][i] - m1 - x[s][i] * dot);
       if (a.ds_in) {
         float in[8];
-        load8<VEC>(a.ds_in + base + c, n, in);
+        load8(a.ds_in + base + c, n, in);
 #pragma unroll
         for (int i = 0; i < 8; i++) o[i] += in[i];
       }
-      store8<VEC>(a.ds + base + c, n, o);
-      if (a.lp) store8<VEC>(a.lp + base + c, n, o);
+      store8(a.ds + base + c, n, o);
+      if (a.lp) store8(a.lp + base + c, n, o);
     }
   }
   float* out = a.partial + (int64_t)blockIdx.x * a.d;
   if (NT == 64) {   // the four wavefronts' sums, in their order
     if (w)
 #pragma unroll
-      for (int s = 0; s < NORM_RUNS; s++) store8<true>(parts[w - 1] + 8 * (t + NT * s), 8, dg[s]);
+      for (int s = 0; s < NORM_RUNS; s++) __builtin_memcpy(parts[w - 1] + 8 * (t + NT * s), dg[s], 32);
     __syncthreads();
     if (w) return;
 #pragma unroll
@@ -191,28 +191,37 @@ __global__ __launch_bounds__(NT == 64 ? 256 : NT) void norm_bwd_kernel(NormBwdAr
 #pragma unroll
       for (int j = 0; j < 3; j++) {
         float o[8];
-        load8<true>(parts[j] + 8 * (t + NT * s), 8, o);
+        load8(parts[j] + 8 * (t + NT * s), 8, o);
 #pragma unroll
         for (int i = 0; i < 8; i++) dg[s][i] += o[i];
       }
   }
 #pragma unroll
-  for (int s = 0; s < NORM_RUNS; s++) store8<VEC>(out + 8 * (t + NT * s), a.d - 8 * (t + NT * s), dg[s]);
+  for (int s = 0; s < NORM_RUNS; s++) store8(out + 8 * (t + NT * s), a.d - 8 * (t + NT * s), dg[s]);
 }
 
-// dgain = the sum of the blocks' rows, in the order of the blocks: 64 columns a workgroup, 16 groups of lanes each with every 16th row
+// dgain = the sum of the blocks' rows, in the order of the blocks: 16 columns a workgroup, 64 groups of lanes each with every 64th row
 __global__ __launch_bounds__(1024) void norm_dgain_kernel(const float* __restrict__ partial, float* __restrict__ dgain, int blocks, int d) {
-  __shared__ float sh[16][64];
-  const int c = blockIdx.x * 64 + (threadIdx.x & 63), g = threadIdx.x >> 6;
+  __shared__ float sh[64][17];
+  const int lc = threadIdx.x & 15, c = blockIdx.x * 16 + lc, g = threadIdx.x >> 4;
   float s = 0.0f;
-  if (c < d)
-    for (int b = g; b < blocks; b += 16) s += partial[(int64_t)b * d + c];
-  sh[g][threadIdx.x & 63] = s;
-  __syncthreads();
-  if (g == 0 && c < d) {
+  if (c < d) {
+    float v[8];   // blocks <= 512
 #pragma unroll
-    for (int i = 1; i < 16; i++) s += sh[i][threadIdx.x];
-    dgain[c] = s;
+    for (int i = 0; i < 8; i++) v[i] = g + 64 * i < blocks ? partial[(int64_t)(g + 64 * i) * d + c] : 0.0f;
+#pragma unroll
+    for (int i = 0; i < 8; i++) s += v[i];
+  }
+  sh[g][lc] = s;
+  __syncthreads();
+  if (threadIdx.x < 64) {   // lane g2 * 16 + lc: groups 16 g2 .. + 15, and then the four sums
+    const int g2 = threadIdx.x >> 4;
+    float r = 0.0f;
+#pragma unroll
+    for (int i = 0; i < 16; i++) r += sh[16 * g2 + i][lc];
+    r += __shfl_xor(r, 16, 64);
+    r += __shfl_xor(r, 32, 64);
+    if (threadIdx.x < 16 && c < d) dgain[c] = r;
   }
 }
 
@@ -222,20 +231,18 @@ __global__ __launch_bounds__(1024) void norm_dgain_kernel(const float* __restric
 
 using namespace als;
 
-// Launches KERNEL<T, NT, VEC, CENTER> for a row of d
-#define ALS_NORM_VC(KERNEL, T, NT, GRID) \
+// Launches KERNEL<T, NT, CENTER> for a row of d
+#define ALS_NORM_C(KERNEL, T, NT, GRID) \
   do { \
     const dim3 grid_(GRID), block_(NT == 64 ? 256 : NT); \
-    if (vec && center) hipLaunchKernelGGL((KERNEL<T, NT, true, true>), grid_, block_, 0, st, a); \
-    else if (vec) hipLaunchKernelGGL((KERNEL<T, NT, true, false>), grid_, block_, 0, st, a); \
-    else if (center) hipLaunchKernelGGL((KERNEL<T, NT, false, true>), grid_, block_, 0, st, a); \
-    else hipLaunchKernelGGL((KERNEL<T, NT, false, false>), grid_, block_, 0, st, a); \
+    if (center) hipLaunchKernelGGL((KERNEL<T, NT, true>), grid_, block_, 0, st, a); \
+    else hipLaunchKernelGGL((KERNEL<T, NT, false>), grid_, block_, 0, st, a); \
   } while (0)
 #define ALS_NORM(KERNEL, T, GRID64, GRID) \
   do { \
-    if (d <= 1024) ALS_NORM_VC(KERNEL, T, 64, GRID64); \
-    else if (d <= 4096) ALS_NORM_VC(KERNEL, T, 256, GRID); \
-    else ALS_NORM_VC(KERNEL, T, 1024, GRID); \
+    if (d <= 1024) ALS_NORM_C(KERNEL, T, 64, GRID64); \
+    else if (d <= 4096) ALS_NORM_C(KERNEL, T, 256, GRID); \
+    else ALS_NORM_C(KERNEL, T, 1024, GRID); \
   } while (0)
 
 static int check_norm(int rows, int d, int norm_kind, const char* what) {
@@ -263,7 +270,6 @@ extern "C" int als_k_norm_fwd(const void* x, int dtype, const float* resid, cons
   a.q = q ? (uint8_t*)q->data : nullptr; a.scale = q ? q->scale : nullptr; a.ld = q ? q->ld : 0; a.ld_scale = q ? q->ld_scale : 0;
   a.format = q ? q->format : 0; a.rstd = rstd; a.rows = rows; a.d = d; a.eps = (float)eps;
   const bool center = norm_kind == ALS_NORM_LAYER;
-  const bool vec = d % 8 == 0 && (((uintptr_t)x | (uintptr_t)resid | (uintptr_t)gain | (uintptr_t)total | (uintptr_t)y) % 16) == 0;
   hipStream_t st = (hipStream_t)stream;
   if (dtype == ALS_DTYPE_BF16) ALS_NORM(norm_fwd_kernel, bf16, (rows + 3) / 4, rows);
   else ALS_NORM(norm_fwd_kernel, float, (rows + 3) / 4, rows);
@@ -292,7 +298,6 @@ extern "C" int als_k_norm_bwd(const void* dy, int dtype, const float* total, con
   a.dy = dy; a.total = total; a.rstd = rstd; a.gain = gain; a.ds_in = ds_in; a.ds = ds; a.lp = (bf16*)ds_lp; a.partial = (float*)ws_dev;
   a.rows = rows; a.d = d;
   const bool center = norm_kind == ALS_NORM_LAYER;
-  const bool vec = d % 8 == 0 && (((uintptr_t)dy | (uintptr_t)total | (uintptr_t)gain | (uintptr_t)ds_in | (uintptr_t)ds | (uintptr_t)ds_lp) % 16) == 0;
   hipStream_t st = (hipStream_t)stream;
   const int blocks = norm_bwd_blocks(rows, d);
   if (rows) {
@@ -300,7 +305,7 @@ extern "C" int als_k_norm_bwd(const void* dy, int dtype, const float* total, con
     else ALS_NORM(norm_bwd_kernel, float, blocks, blocks);
     ALS_CHECK_LAUNCH();
   }
-  hipLaunchKernelGGL(norm_dgain_kernel, dim3((d + 63) / 64), dim3(1024), 0, st, a.partial, dgain, blocks, d);
+  hipLaunchKernelGGL(norm_dgain_kernel, dim3((d + 15) / 16), dim3(1024), 0, st, a.partial, dgain, blocks, d);
   ALS_CHECK_LAUNCH();
   return ALS_OK;
 }
