@@ -1,0 +1,6 @@
+// The tiles of products of e4m3 (A) and e5m2 (B)
+#include "gemm_fp8_kernels.h"
+
+namespace als {
+template int gemm_fp8_launch<0, 1>(Fp8Args, int, Fp8Out, hipStream_t);
+}
