@@ -204,6 +204,13 @@ int als_set_vector(als_ctx* ctx, int which, int worker, const float* host_in);
 int als_sync(als_ctx* ctx, int worker);
 /* Losses of the worker's most recent als_worker_local_steps call (n <= its n_steps). */
 int als_get_losses(als_ctx* ctx, int worker, float* host_out, int n);
+/* Gradient clipping of the local steps that are enqueued from now on: a step's gradient, over all parameters, is multiplied by max_norm / norm if its
+ * norm exceeds max_norm (> 0), before AdamW.  0, as after als_init: off.  ALS_VEC_GRAD keeps the gradient as it was before.  A worker whose
+ * steps are replayed has its graph captured anew: the call then waits for all workers, and is refused
+ * while a measurement hook is in force. */
+int als_set_grad_clip(als_ctx* ctx, double max_norm);
+/* The gradients' norms, before clipping, of the worker's most recent als_worker_local_steps call (n <= its n_steps; 0 if it did not clip). */
+int als_get_grad_norms(als_ctx* ctx, int worker, float* host_out, int n);
 /* Number of Alg. 3 events applied so far (t). */
 int64_t als_server_t(als_ctx* ctx);
 /* AdamW step count of a worker. */

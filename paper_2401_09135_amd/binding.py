@@ -84,6 +84,8 @@ lib.als_get_vector.argtypes = [_P, C.c_int, C.c_int, _P]
 lib.als_set_vector.argtypes = [_P, C.c_int, C.c_int, _P]
 lib.als_sync.argtypes = [_P, C.c_int]
 lib.als_get_losses.argtypes = [_P, C.c_int, _P, C.c_int]
+lib.als_set_grad_clip.argtypes = [_P, C.c_double]
+lib.als_get_grad_norms.argtypes = [_P, C.c_int, _P, C.c_int]
 lib.als_server_t.restype = C.c_int64
 lib.als_server_t.argtypes = [_P]
 lib.als_worker_adam_steps.restype = C.c_int64
@@ -288,6 +290,16 @@ class Context:
     def get_losses(self, worker: int, n: int) -> np.ndarray:
         out = np.zeros(n, dtype=np.float32)
         _check(lib.als_get_losses(self._ctx, worker, _np_ptr(out), n))
+        return out
+
+    def set_grad_clip(self, max_norm: float) -> None:
+        """Clips the gradients of the local steps that follow to this norm; 0 turns it off."""
+        _check(lib.als_set_grad_clip(self._ctx, float(max_norm)))
+
+    def get_grad_norms(self, worker: int, n: int) -> np.ndarray:
+        """Norms, before clipping, of the gradients of the worker's last worker_local_steps call."""
+        out = np.zeros(n, dtype=np.float32)
+        _check(lib.als_get_grad_norms(self._ctx, worker, _np_ptr(out), n))
         return out
 
     @property

@@ -245,8 +245,10 @@ __device__ __forceinline__ float clip_coefficient(float norm, float max_norm) { 
 struct ClipArgs { const float* norm; float max_norm, rest1, rest2; };   // rest: 1 - beta
 int adamw_clip(float* theta, const float* grad, float* m, float* v, bf16* lp, int64_t P, int64_t P_decay, const AdamArgs& a, const ClipArgs& clip,
                hipStream_t st, StepState* ss = nullptr);
-// the square root of the sum of the squares of n tensors (grad_norm.hip); partial: scratch of als_k_grad_norm_ws_bytes
-int grad_norm(int n, const void* const* grads, const int64_t* numel, const int32_t* dtypes, float* norm_out, double* partial, hipStream_t st);
+// the square root of the sum of the squares of n tensors (grad_norm.hip); partial: scratch of als_k_grad_norm_ws_bytes.  Also left in log, or,
+// of a step that is replayed, log_offset behind where that step leaves its loss.
+int grad_norm(int n, const void* const* grads, const int64_t* numel, const int32_t* dtypes, float* norm_out, double* partial, hipStream_t st,
+              float* log = nullptr, const StepState* ss = nullptr, int64_t log_offset = 0);
 
 #define ALS_DN_MAX_GROUP 16
 struct DnGroup {

@@ -25,7 +25,8 @@ struct Worker {
   float *dxa, *dxb, *dtmp, *Dbuf, *partial;
   void *dx_lp, *dff, *d_o, *dqkv;
   // pinned; a step writes its loss there itself: a copy per call cost the host as much as several launches
-  float* losses_host; float* losses_dev;   // losses_dev: its address on the device
+  float* losses_host; float* losses_dev;   // losses_dev: its address on the device; max_local_steps losses, then as many gradient norms
+  double* norm_partial; float* norm;       // of the clipped steps, in the arena
   int32_t *sort_offset, *sort_rank, *sort_pos;
   float* splitk_ws; size_t splitk_bytes;
   float* head_ws; size_t head_ws_bytes;   // split-K scratch of the output matrix's input gradient
@@ -38,6 +39,7 @@ struct Worker {
   std::vector<DwProblem> dw_probs; std::vector<DwItem> dw_items; std::vector<DwSplitTile> dw_split;
   DwPlan dw_plan;
   int64_t adam_n; int last_n;
+  int last_norms;     // of these last_n steps, those whose gradient's norm was taken: all or none
   int64_t t_restart;  // server event count when this replica last (re)started
   hipStream_t stream; hipEvent_t done_ev, ready_ev;
   hipStream_t done_st, ready_st;   // where these were last recorded
@@ -58,6 +60,8 @@ struct als_ctx {
   char capture_error[512];   // why a step could not be captured, empty if none failed
   hipEvent_t server_ev; hipStream_t server_st;
   bool bf; bool allow_mfma;
+  bool replays;             // steps are to run as graphs
+  float max_norm;           // gradients of local steps are clipped to it; 0: they are not, and their norm is not taken
   bool grouped_dw;   // the layers' weight gradients run as one grouped launch at the end of the backward pass
   bool list_dw;      // the same, the output matrix's too, where they have no aligned kernel
   int T;
@@ -113,6 +117,8 @@ void carve(als_ctx* c, Carver& cv) {
     w.theta = cv.f32(P); w.start = cv.f32(P); w.adam_m = cv.f32(P); w.adam_v = cv.f32(P);
     w.grad = cv.f32(P);
     w.state = (StepState*)cv.take(sizeof(StepState));
+    w.norm_partial = (double*)cv.take(als_k_grad_norm_ws_bytes(1, &P));
+    w.norm = cv.f32(1);
     w.lp = bf ? (bf16*)cv.take((size_t)P * 2) : nullptr;
     int L = g.n_layers;
     w.x.resize(L + 1); w.xm.resize(L); w.rstd1.resize(L); w.rstd2.resize(L); w.lse.resize(L);
@@ -297,6 +303,18 @@ int check_ctx_worker(als_ctx* ctx, int worker) {
   return ALS_OK;
 }
 
+// The update behind a backward pass: the worker's step s, or that of *ss.  A step that clips reads the gradient once more, for its norm; the
+// coefficient is applied where AdamW reads it anyway.
+int update(als_ctx* ctx, Worker& w, int s, const AdamArgs& a, hipStream_t st, StepState* ss) {
+  const Layout& L = ctx->L;
+  if (ctx->max_norm == 0.0f) return adamw(w.theta, w.grad, w.adam_m, w.adam_v, w.lp, L.P, L.P_decay, a, st, ss);
+  const void* grad = w.grad;
+  const int64_t norms = ctx->cfg.max_local_steps;   // behind the losses
+  RUN(grad_norm(1, &grad, &L.P, nullptr, w.norm, w.norm_partial, st, ss ? nullptr : w.losses_dev + norms + s, ss, norms));
+  return adamw_clip(w.theta, w.grad, w.adam_m, w.adam_v, w.lp, L.P, L.P_decay, a,
+                    ClipArgs{w.norm, ctx->max_norm, (float)(1.0 - ctx->cfg.adam_beta1), (float)(1.0 - ctx->cfg.adam_beta2)}, st, ss);
+}
+
 std::atomic<bool> g_fail_capture{false};
 
 // The step of one worker as a graph, captured on a stream of its own (nothing runs there).  On any failure the context goes on
@@ -310,7 +328,7 @@ void capture_step(als_ctx* ctx, Worker& w, hipStream_t cs) {
   if (e == hipSuccess) {
     rc = forward(ctx, w, nullptr, cs, w.state);
     if (!rc) rc = backward(ctx, w, nullptr, 0, nullptr, cs, w.state);
-    if (!rc) rc = adamw(w.theta, w.grad, w.adam_m, w.adam_v, w.lp, ctx->L.P, ctx->L.P_decay, AdamArgs{}, cs, w.state);
+    if (!rc) rc = update(ctx, w, 0, AdamArgs{}, cs, w.state);
     if (!rc && g_fail_capture.load()) rc = set_error(ALS_ERR_HIP, "capture made to fail");
     e = hipStreamEndCapture(cs, &graph);
   }
@@ -322,6 +340,17 @@ void capture_step(als_ctx* ctx, Worker& w, hipStream_t cs) {
   }
   if (graph) (void)hipGraphDestroy(graph);
   (void)hipGetLastError();
+}
+
+void capture_steps(als_ctx* ctx) {
+  ctx->capture_error[0] = 0;
+  hipStream_t cs = nullptr;
+  if (hipStreamCreateWithFlags(&cs, hipStreamNonBlocking) == hipSuccess) {
+    for (Worker& w : ctx->w) capture_step(ctx, w, cs);
+    (void)hipStreamDestroy(cs);
+  } else {
+    snprintf(ctx->capture_error, sizeof ctx->capture_error, "%s", hipGetErrorString(hipGetLastError()));
+  }
 }
 
 // Whether the launches of the workers' steps hold the host longer than the chip (streams: different ones that the workers run on).  A launch
@@ -403,6 +432,8 @@ extern "C" int als_init(const als_config* cfg, void* arena, size_t arena_bytes, 
   c->allow_mfma = !(cfg->flags & 1);
   c->T = cfg->batch * cfg->seq_len;
   c->t = 0;
+  c->max_norm = 0.0f;
+  c->replays = false;
   c->capture_error[0] = 0;
   Carver cv{(char*)arena, 0};
   carve(c, cv);
@@ -431,11 +462,11 @@ extern "C" int als_init(const als_config* cfg, void* arena, size_t arena_bytes, 
   for (size_t i = 0; i < c->w.size(); i++) {
     Worker& w = c->w[i];
     w.stream = (hipStream_t)streams[i % n_streams];
-    w.adam_n = 0; w.last_n = 0; w.t_restart = 0;
+    w.adam_n = 0; w.last_n = 0; w.last_norms = 0; w.t_restart = 0;
     w.ready_st = w.done_st = w.stream;
     if (hipEventCreateWithFlags(&w.done_ev, hipEventDisableTiming) != hipSuccess ||
         hipEventCreateWithFlags(&w.ready_ev, hipEventDisableTiming) != hipSuccess ||
-        hipHostMalloc((void**)&w.losses_host, (size_t)cfg->max_local_steps * 4, hipHostMallocDefault) != hipSuccess ||
+        hipHostMalloc((void**)&w.losses_host, (size_t)cfg->max_local_steps * 2 * 4, hipHostMallocDefault) != hipSuccess ||
         hipHostGetDevicePointer((void**)&w.losses_dev, w.losses_host, 0) != hipSuccess)
       return fail(set_error(ALS_ERR_HIP, "als_init: event or pinned-buffer creation failed"));
     if (hipMemsetAsync(w.adam_m, 0, (size_t)P * 4, w.stream) != hipSuccess ||
@@ -451,15 +482,8 @@ extern "C" int als_init(const als_config* cfg, void* arena, size_t arena_bytes, 
   if (hipEventRecord(c->server_ev, s0) != hipSuccess) return fail(set_error(ALS_ERR_HIP, "hipEventRecord failed"));
   rc = sync_all(c);
   if (rc) return fail(rc);
-  if (replay_pays(*cfg, used_streams(*cfg, streams, n_streams)) && !gemm_hooks_active()) {
-    hipStream_t cs = nullptr;
-    if (hipStreamCreateWithFlags(&cs, hipStreamNonBlocking) == hipSuccess) {
-      for (Worker& w : c->w) capture_step(c, w, cs);
-      (void)hipStreamDestroy(cs);
-    } else {
-      snprintf(c->capture_error, sizeof c->capture_error, "%s", hipGetErrorString(hipGetLastError()));
-    }
-  }
+  c->replays = replay_pays(*cfg, used_streams(*cfg, streams, n_streams)) && !gemm_hooks_active();
+  if (c->replays) capture_steps(c);
   *out = c;
   return ALS_OK;
 }
@@ -533,9 +557,10 @@ extern "C" int als_worker_local_steps(als_ctx* ctx, int worker, int n_steps, con
     RUN(forward(ctx, w, tok, w.stream, nullptr));
     RUN(backward(ctx, w, tok, s, w.losses_dev + s, w.stream, nullptr));
     w.adam_n += 1;
-    RUN(adamw(w.theta, w.grad, w.adam_m, w.adam_v, w.lp, ctx->L.P, ctx->L.P_decay, adam_args(s, w.adam_n), w.stream));
+    RUN(update(ctx, w, s, adam_args(s, w.adam_n), w.stream, nullptr));
   }
   w.last_n = n_steps;
+  w.last_norms = ctx->max_norm > 0 ? n_steps : 0;
   ALS_HIP(hipEventRecord(w.done_ev, w.stream));
   w.done_st = w.stream;
   if (loss_host) {
@@ -715,6 +740,36 @@ extern "C" int als_get_losses(als_ctx* ctx, int worker, float* host_out, int n) 
   if (!host_out || n < 0 || n > w.last_n) return set_error(ALS_ERR_INVALID, "n outside 0..%d", w.last_n);
   ALS_HIP(hipStreamSynchronize(w.stream));
   memcpy(host_out, w.losses_host, (size_t)n * 4);
+  return ALS_OK;
+}
+
+extern "C" int als_get_grad_norms(als_ctx* ctx, int worker, float* host_out, int n) {
+  int rc = check_ctx_worker(ctx, worker);
+  if (rc) return rc;
+  Worker& w = ctx->w[worker];
+  if (!host_out || n < 0 || n > w.last_norms) return set_error(ALS_ERR_INVALID, "n outside 0..%d (norms are taken of steps that clip)", w.last_norms);
+  ALS_HIP(hipStreamSynchronize(w.stream));
+  memcpy(host_out, w.losses_host + ctx->cfg.max_local_steps, (size_t)n * 4);
+  return ALS_OK;
+}
+
+extern "C" int als_set_grad_clip(als_ctx* ctx, double max_norm) {
+  if (!ctx) return set_error(ALS_ERR_INVALID, "context is null");
+  const float f = (float)max_norm;
+  if (max_norm != 0 && (!(f > 0) || max_norm > 3.4e38)) return set_error(ALS_ERR_INVALID, "als_set_grad_clip: max_norm must be 0, or positive and finite");
+  for (Worker& w : ctx->w) RUN(check_not_captured(w.stream));
+  if (f == ctx->max_norm) return ALS_OK;
+  if (ctx->replays && gemm_hooks_active()) return set_error(ALS_ERR_INVALID, "als_set_grad_clip: steps cannot be captured while kernels are measured or chosen by hand");
+  if (ctx->replays) {   // the graphs hold the old setting; steps that run as one are waited for
+    RUN(sync_all(ctx));
+    for (Worker& w : ctx->w) {
+      ALS_HIP(hipEventSynchronize(w.done_ev));
+      if (w.step_graph) (void)hipGraphExecDestroy(w.step_graph);
+      w.step_graph = nullptr;
+    }
+  }
+  ctx->max_norm = f;
+  if (ctx->replays) capture_steps(ctx);
   return ALS_OK;
 }
 

@@ -117,7 +117,8 @@ __global__ __launch_bounds__(256) void grad_squares_kernel(GradTable t, double* 
   if (threadIdx.x == 0) partial[blockIdx.x] = sh[0] + sh[1] + sh[2] + sh[3];
 }
 
-__global__ __launch_bounds__(1024) void grad_norm_kernel(const double* __restrict__ partial, int64_t n, float* __restrict__ norm) {
+__global__ __launch_bounds__(1024) void grad_norm_kernel(const double* __restrict__ partial, int64_t n, float* __restrict__ norm, float* log, const StepState* ss,
+                                                         int64_t log_offset) {
   __shared__ double sh[16];
   double s = 0.0;
   for (int64_t i = threadIdx.x; i < n; i += 1024) s += partial[i];
@@ -126,7 +127,10 @@ __global__ __launch_bounds__(1024) void grad_norm_kernel(const double* __restric
   __syncthreads();
   if (threadIdx.x == 0) {
     for (int i = 1; i < 16; i++) s += sh[i];
-    norm[0] = (float)sqrt(s);
+    const float root = (float)sqrt(s);
+    norm[0] = root;
+    if (ss) log = ss->loss_out + ss->step + log_offset;
+    if (log) log[0] = root;
   }
 }
 
@@ -212,7 +216,8 @@ int check_list_ws(int n, const int64_t* numel, const void* ws, size_t ws_bytes, 
 
 }  // namespace
 
-int grad_norm(int n, const void* const* grads, const int64_t* numel, const int32_t* dtypes, float* norm_out, double* partial, hipStream_t st) {
+int grad_norm(int n, const void* const* grads, const int64_t* numel, const int32_t* dtypes, float* norm_out, double* partial, hipStream_t st, float* log,
+              const StepState* ss, int64_t log_offset) {
   int64_t count = 0;
   int rc = for_launches(n, grads, nullptr, numel, dtypes, [&](const GradTable& t, int blocks, int64_t p0) {
     hipLaunchKernelGGL(grad_squares_kernel, dim3(blocks), dim3(256), 0, st, t, partial + p0);
@@ -221,7 +226,7 @@ int grad_norm(int n, const void* const* grads, const int64_t* numel, const int32
     return ALS_OK;
   });
   if (rc) return rc;
-  hipLaunchKernelGGL(grad_norm_kernel, dim3(1), dim3(1024), 0, st, partial, count, norm_out);
+  hipLaunchKernelGGL(grad_norm_kernel, dim3(1), dim3(1024), 0, st, partial, count, norm_out, log, ss, log_offset);
   ALS_CHECK_LAUNCH();
   return ALS_OK;
 }

@@ -10,11 +10,13 @@ from .binding import Config, Context, dylu_schedule
 
 def run_async(w: dict, theta0: np.ndarray, make_stream, n_events: int | None = None, flags: int = 0,
               ctx: Context | None = None, collect_losses: bool = True, lr=None, rule: dict | None = None,
-              on_group=None):
+              on_group=None, grad_clip: float | None = None):
     """w: workload dict (als_inputs.workload); make_stream(i) -> object with take(n) giving
     int32 [n,B,S+1] token batches for worker i.  Returns dict like the oracle's run.
     on_group(ctx, index of the group's last event): optional observer called after every applied
-    group of sync events (before its workers are given new rounds)."""
+    group of sync events (before its workers are given new rounds).
+    grad_clip: norm that the local steps' gradients are clipped to, 0 for no clipping (None: as ctx is set); the
+    norms before clipping are then in the result's grad_norms."""
     import torch
     n_events = w["n_events"] if n_events is None else n_events
     steps, ev_w, ev_t, ev_g = dylu_schedule(w["speeds"], w["H"], w["tau_grace"], n_events)
@@ -24,7 +26,9 @@ def run_async(w: dict, theta0: np.ndarray, make_stream, n_events: int | None = N
         ctx = Context(cfg, theta0)
     k = w["k"]
     streams = [make_stream(i) for i in range(k)]
-    losses = [[] for _ in range(k)]
+    losses, norms = [[] for _ in range(k)], [[] for _ in range(k)]
+    if grad_clip is not None:
+        ctx.set_grad_clip(grad_clip)
     pending = [0] * k
     lr = w["lr"] if lr is None else lr
 
@@ -36,6 +40,8 @@ def run_async(w: dict, theta0: np.ndarray, make_stream, n_events: int | None = N
     def harvest(i):
         if collect_losses and pending[i]:
             losses[i].extend(ctx.get_losses(i, pending[i]).tolist())
+            if grad_clip:
+                norms[i].extend(ctx.get_grad_norms(i, pending[i]).tolist())
         pending[i] = 0
 
     for i in range(k):
@@ -63,5 +69,5 @@ def run_async(w: dict, theta0: np.ndarray, make_stream, n_events: int | None = N
     for i in range(k):
         harvest(i)
     out = dict(theta=ctx.get_vector("theta"), m=ctx.get_vector("momentum"), delta=ctx.get_vector("delta"),
-               t=ctx.server_t, losses=losses, steps=steps, ev_worker=ev_w, ev_time=ev_t, ev_group_end=ev_g, ctx=ctx)
+               t=ctx.server_t, losses=losses, grad_norms=norms, steps=steps, ev_worker=ev_w, ev_time=ev_t, ev_group_end=ev_g, ctx=ctx)
     return out

@@ -1,6 +1,7 @@
 """What the operators for 8-bit layers and clipping refuse: checked before any work reaches the GPU, so these run without one."""
 import ctypes as C
 
+import numpy as np
 import pytest
 import torch
 
@@ -177,3 +178,9 @@ def test_product_hook_refuses(tile, shares):
 @pytest.mark.parametrize("bad", [dict(ldc=(1 << 26) + 1), dict(r=P16 + 64, ldr=(1 << 26) + 1), dict(N=(1 << 20) + 1, ldc=1 << 21), dict(a=dict(ld=(1 << 23) + 16)), dict(b=dict(ld_scale=(1 << 23) + 4))])
 def test_gemm_refuses_what_its_addresses_do_not_reach(bad):
     assert gemm(**bad) == INVALID
+
+
+def test_clipping_of_local_steps_needs_a_context():
+    out = np.zeros(1, dtype=np.float32)
+    assert A.lib.als_set_grad_clip(None, 1.0) != 0 and b"null" in A.lib.als_last_error()
+    assert A.lib.als_get_grad_norms(None, 0, out.ctypes.data, 1) != 0 and b"null" in A.lib.als_last_error()

@@ -104,7 +104,6 @@ def test_quantiser_rounds_every_fp32_near_every_8_bit_value(fmt):
     x = x[x.abs() <= TOP[fmt]]
     rows = -(-x.numel() // 127)
     m = torch.full((rows, 128), TOP[fmt])
-    m[:, 1:].reshape(-1)
     m[:, 1:] = torch.cat([x, torch.zeros(rows * 127 - x.numel())]).view(rows, 127)
     q = A.Fp8.empty(rows, 128, fmt)
     A.k_quant_fp8(m.to(DEV), q)
