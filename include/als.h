@@ -292,7 +292,9 @@ int als_k_attention_bwd(const void* qkv, const void* o, const void* d_o, const f
  * scale [ceil(rows / block_rows), ceil(cols / 128)], rows ld_scale bytes apart.  An element stands for its 8-bit value times its block's scale.
  * ld must be a multiple of 16 and at least cols, ld_scale a multiple of 4 and at least ceil(cols / 128); data 16-byte,
  * scale 4-byte aligned; the last row is ld bytes long like the others, the last scale row ld_scale: what lies behind the columns may be
- * read and is never used, and never written. */
+ * read and is never used, and never written.
+ * The calls of this section and the next enqueue work on `stream`, allocate nothing and may be captured into graphs.  Where nothing else is said, outputs and workspaces
+ * overlap no other buffer of the call, and no buffer that another call uses at the same time: calls that may run side by side, as two graphs, have workspaces of their own. */
 #define ALS_FP8_E4M3 0
 #define ALS_FP8_E5M2 1
 typedef struct als_fp8 {
@@ -306,10 +308,10 @@ typedef struct als_fp8 {
  * if qt is not) transposed, [cols, rows], with blocks of its own along its own rows.  The scale of a block is the least power of two, at least
  * 2^-127, under which its largest finite magnitude is at most the format's largest value, and 1 for a block without any; every element is divided
  * by it, which is exact, and rounded to the nearest value, ties to even.  What is not finite is not counted in and shows: NaN becomes NaN, an infinity becomes
- * NaN in e4m3 and stays one in e5m2.  q and qt may have different formats and block_rows; the three must not overlap. */
+ * NaN in e4m3 and stays one in e5m2.  rows, cols <= 2^30, and fewer than 2^24 blocks of 128 x 128.  q and qt may have different formats and block_rows; the three must not overlap. */
 int als_k_quant_fp8(const void* x, int dtype, int rows, int cols, int64_t ldx, const als_fp8* q, const als_fp8* qt, void* stream);
 
-/* Norm of x + resid in one pass, for rows of d <= 16384 elements: total = x + resid; y = total rstd gain (ALS_NORM_RMS; ALS_NORM_LAYER: total
+/* Norm of x + resid in one pass, for up to 2^30 rows of d <= 16384 elements: total = x + resid; y = total rstd gain (ALS_NORM_RMS; ALS_NORM_LAYER: total
  * minus its mean), rstd = 1 / sqrt(mean of squares + eps).  x in dtype, resid and total fp32, all [rows, d] without padding; resid and total are both null
  * (then total is x) or neither; total may be resid, or x in fp32.  y (bf16 [rows, d]) and q (8 bits with block_rows 1, formed from y before its rounding) may
  * be null, not both.  rstd [rows] is what the backward pass takes. */
@@ -327,7 +329,8 @@ int als_k_norm_bwd(const void* dy, int dtype, const float* total, const float* r
  * [K, N] is taken as its transposed form), any two formats and block_rows.  fp32 results: exact products of elements from 2^-126 to 2^127, summed in fp32.  bf16
  * results: the 8-bit matrix instruction, at up to twice the rate; it sums in fp32 too, but among 8 neighbours in K a product under 2^-13 of the largest may be
  * lost (1.5e-5 of a sum of random signs; a rounding to bf16 is up to 4e-3).  C [M, N] in out_dtype, rows ldc elements
- * apart; R (fp32, rows ldr apart) may be null, and may be C itself if that is fp32.  K = 0 gives R or zeros.
+ * apart; R (fp32, rows ldr apart) may be null, and may be C itself if that is fp32 and ldr is ldc.  K = 0 gives R or zeros.  M, K <= 2^30, N <= 2^20, ld and ld_scale
+ * <= 2^23, ldc and ldr <= 2^26.
  * ws_dev (256-byte aligned, may be null): scratch for the partial sums of products that are split along K; als_k_gemm_fp8_ws_bytes is what
  * one takes at most, with less it is split less.  Results do not depend on timing. */
 size_t als_k_gemm_fp8_ws_bytes(int M, int N, int K);

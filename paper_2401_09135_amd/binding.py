@@ -539,7 +539,7 @@ def _rows_of(what, t, multiple):
         return t.data_ptr(), -(-cols // multiple) * multiple
     ld, unit = t.stride()
     if rows == 1:
-        ld = max(ld, -(-cols // multiple) * multiple)
+        ld = -(-cols // multiple) * multiple
     p = t.data_ptr()
     if (unit != 1 and cols > 1) or ld < cols or ld % multiple or p % multiple:
         raise AlsError(f"{what}: columns must be contiguous, the start and the row stride multiples of {multiple} bytes")
@@ -628,10 +628,16 @@ def k_quant_fp8(x, q=None, qt=None, stream=None):
 NORM_KINDS = {"rms": 0, "layer": 1}
 
 
+def _norm_args(what, x, norm):
+    if x.dim() != 2 or norm not in NORM_KINDS:
+        raise AlsError(f"{what}: expected a matrix and norm 'rms' or 'layer', got {tuple(x.shape)} and {norm!r}")
+    return x.shape
+
+
 def k_norm_fwd(x, gain, resid=None, total=None, y=None, q=None, rstd=None, norm="rms", eps=1e-5, stream=None):
     """als_k_norm_fwd: total = x + resid and its norm, in bf16 (y) and / or 8 bits (q, Fp8); x [rows, d] fp32 or bf16."""
     what, f32 = "k_norm_fwd", torch.float32
-    rows, d = x.shape
+    rows, d = _norm_args(what, x, norm)
     n = rows * d
     if q is not None and q.shape != (rows, d):
         raise AlsError("k_norm_fwd: q must be [rows, d]")
@@ -648,7 +654,7 @@ def k_norm_bwd_ws_bytes(rows: int, d: int) -> int:
 def k_norm_bwd(dy, total, rstd, gain, ds, dgain, ws, ds_in=None, ds_lp=None, norm="rms", stream=None):
     """als_k_norm_bwd: ds (and its bf16 copy ds_lp) and dgain from dy [rows, d] (fp32 or bf16) and what k_norm_fwd left."""
     what, f32 = "k_norm_bwd", torch.float32
-    rows, d = dy.shape
+    rows, d = _norm_args(what, dy, norm)
     n = rows * d
     dev = _device(what, dy, total, rstd, gain, ds, dgain, ws, ds_in, ds_lp)
     p, code = _either(what, dy)

@@ -238,7 +238,7 @@ int launch_quant(const T* x, int rows, int cols, int64_t ldx, const als_fp8* q, 
     return f ? Fp8Out{(uint8_t*)f->data, f->scale, f->ld, f->ld_scale, f->format, f->block_rows} : Fp8Out{};
   };
   const int64_t tr = fp8_blocks(rows), tc = fp8_blocks(cols);
-  if (tr * tc > 0x7fffffff) return set_error(ALS_ERR_INVALID, "als_k_quant_fp8: matrix too large");
+  if (tr * tc >= 1 << 24) return set_error(ALS_ERR_INVALID, "als_k_quant_fp8: matrix of 2^24 blocks of 128 x 128 or more");
 #define ALS_QUANT(A, B) hipLaunchKernelGGL((quant_fp8_kernel<T, A, B>), dim3((unsigned)(tr * tc)), dim3(256), 0, st, x, rows, cols, ldx, out(q), out(qt), (int)tc)
   if (q && qt) ALS_QUANT(true, true);
   else if (q) ALS_QUANT(true, false);

@@ -154,7 +154,7 @@ extern "C" int als_k_set_gemm_fp8(int tile, int shares) {
 }
 
 extern "C" int als_k_gemm_fp8_route(int M, int N, int K, int out_dtype, size_t ws_bytes, int* tile_out, int* shares_out) {
-  if (M <= 0 || N <= 0 || K < 0 || !tile_out || !shares_out) return set_error(ALS_ERR_INVALID, "als_k_gemm_fp8_route: null argument or bad size");
+  if (M <= 0 || N <= 0 || K < 0 || M > 1 << 30 || N > 1 << 20 || K > 1 << 30 || !tile_out || !shares_out) return set_error(ALS_ERR_INVALID, "als_k_gemm_fp8_route: null argument or bad size");
   const Fp8Plan p = fp8_plan(M, N, K, out_dtype == ALS_DTYPE_F32, ws_bytes);
   *tile_out = p.tile; *shares_out = p.nsplit;
   return ALS_OK;

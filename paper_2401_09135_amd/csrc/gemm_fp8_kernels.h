@@ -240,7 +240,7 @@ __device__ __forceinline__ void wait_loads() {   // all but the N youngest loads
 __device__ __forceinline__ __amdgpu_buffer_rsrc_t fp8_buffer(const uint8_t* p) {
   const uint64_t u = (uint64_t)(uintptr_t)p;
   const uint64_t s = (uint64_t)(unsigned)fp8_uniform((int)(unsigned)u) | (uint64_t)(unsigned)fp8_uniform((int)(unsigned)(u >> 32)) << 32;
-  return __builtin_amdgcn_make_buffer_rsrc((void*)(uintptr_t)s, 0, 0x7fffffff, 0x00027000);
+  return __builtin_amdgcn_make_buffer_rsrc((void*)(uintptr_t)s, 0, -1, 0x00027000);
 }
 
 // Tile `id` of the launch: its place in C, its K slices, and where its share's partial sums begin.  Workgroups are dealt to the XCDs in turn: each XCD gets

@@ -9,6 +9,7 @@ namespace als {
 namespace {
 
 constexpr int NORM_MAX_D = 16384;
+constexpr int NORM_LAUNCH_ROWS = 1 << 21;   // of a launch of the forward pass: a grid has fewer than 2^32 threads
 
 __device__ __forceinline__ float norm_wave_sum(float v) {
 #pragma unroll
@@ -246,7 +247,7 @@ using namespace als;
   } while (0)
 
 static int check_norm(int rows, int d, int norm_kind, const char* what) {
-  if (rows < 0 || d < 1 || d > NORM_MAX_D) return set_error(ALS_ERR_INVALID, "%s: rows must be >= 0 and d in 1..%d", what, NORM_MAX_D);
+  if (rows < 0 || rows > 1 << 30 || d < 1 || d > NORM_MAX_D) return set_error(ALS_ERR_INVALID, "%s: rows must be in 0..2^30 and d in 1..%d", what, NORM_MAX_D);
   if (norm_kind != ALS_NORM_RMS && norm_kind != ALS_NORM_LAYER) return set_error(ALS_ERR_INVALID, "%s: unknown norm_kind", what);
   return ALS_OK;
 }
@@ -265,20 +266,26 @@ extern "C" int als_k_norm_fwd(const void* x, int dtype, const float* resid, cons
   if (!x || !gain || !rstd) return set_error(ALS_ERR_INVALID, "als_k_norm_fwd: null argument");
   if ((uintptr_t)x % (dtype == ALS_DTYPE_BF16 ? 2 : 4) || ((uintptr_t)resid | (uintptr_t)gain | (uintptr_t)total | (uintptr_t)rstd) % 4 || (uintptr_t)y % 2)
     return set_error(ALS_ERR_INVALID, "als_k_norm_fwd: a tensor is not aligned to its type");
-  NormFwdArgs a;
-  a.x = x; a.resid = resid; a.gain = gain; a.total = total; a.y = (bf16*)y;
-  a.q = q ? (uint8_t*)q->data : nullptr; a.scale = q ? q->scale : nullptr; a.ld = q ? q->ld : 0; a.ld_scale = q ? q->ld_scale : 0;
-  a.format = q ? q->format : 0; a.rstd = rstd; a.rows = rows; a.d = d; a.eps = (float)eps;
   const bool center = norm_kind == ALS_NORM_LAYER;
   hipStream_t st = (hipStream_t)stream;
-  if (dtype == ALS_DTYPE_BF16) ALS_NORM(norm_fwd_kernel, bf16, (rows + 3) / 4, rows);
-  else ALS_NORM(norm_fwd_kernel, float, (rows + 3) / 4, rows);
-  ALS_CHECK_LAUNCH();
+  for (int row0 = 0; row0 < rows; row0 += NORM_LAUNCH_ROWS) {
+    const int n = rows - row0 < NORM_LAUNCH_ROWS ? rows - row0 : NORM_LAUNCH_ROWS;
+    const int64_t at = (int64_t)row0 * d;
+    NormFwdArgs a;
+    a.x = (const char*)x + at * (dtype == ALS_DTYPE_BF16 ? 2 : 4);
+    a.resid = resid ? resid + at : nullptr; a.gain = gain; a.total = total ? total + at : nullptr; a.y = y ? (bf16*)y + at : nullptr;
+    a.q = q ? (uint8_t*)q->data + row0 * q->ld : nullptr; a.scale = q ? q->scale + row0 * q->ld_scale : nullptr;
+    a.ld = q ? q->ld : 0; a.ld_scale = q ? q->ld_scale : 0; a.format = q ? q->format : 0;
+    a.rstd = rstd + row0; a.rows = n; a.d = d; a.eps = (float)eps;
+    if (dtype == ALS_DTYPE_BF16) ALS_NORM(norm_fwd_kernel, bf16, (n + 3) / 4, n);
+    else ALS_NORM(norm_fwd_kernel, float, (n + 3) / 4, n);
+    ALS_CHECK_LAUNCH();
+  }
   return ALS_OK;
 }
 
 extern "C" size_t als_k_norm_bwd_ws_bytes(int rows, int d) {
-  if (rows < 0 || d < 1 || d > NORM_MAX_D) return 0;
+  if (rows < 0 || rows > 1 << 30 || d < 1 || d > NORM_MAX_D) return 0;
   return (size_t)norm_bwd_blocks(rows, d) * d * sizeof(float);
 }
 

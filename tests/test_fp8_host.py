@@ -184,3 +184,44 @@ def test_clipping_of_local_steps_needs_a_context():
     out = np.zeros(1, dtype=np.float32)
     assert A.lib.als_set_grad_clip(None, 1.0) != 0 and b"null" in A.lib.als_last_error()
     assert A.lib.als_get_grad_norms(None, 0, out.ctypes.data, 1) != 0 and b"null" in A.lib.als_last_error()
+
+
+def test_shares_of_many_tiles_are_numbered_or_not_taken():
+    """A tile of a share has a number below 2^32 / tiles: forced shares beyond that are one."""
+    A.set_gemm_fp8(64, 24)
+    try:
+        assert A.gemm_fp8_route(1 << 22, 64, 8192, ws_bytes=1 << 40) == (64, 1)
+        assert A.gemm_fp8_route(1 << 16, 64, 8192, ws_bytes=1 << 40) == (64, 24)
+    finally:
+        A.set_gemm_fp8(0)
+    with pytest.raises(A.AlsError):
+        A.gemm_fp8_route((1 << 30) + 1, 64, 128, ws_bytes=0)
+
+
+@pytest.mark.parametrize("rows,cols", [(1 << 30, 129), (129 << 12, 1 << 20)])
+def test_quant_refuses_more_tiles_than_a_launch_has(rows, cols):
+    f = _Fp8Struct(P16, P16, -(-cols // 16) * 16, -(-cols // 512) * 4, 0, 128)
+    assert lib.als_k_quant_fp8(P16, 1, rows, cols, cols, C.byref(f), None, None) == INVALID
+
+
+def test_norm_refuses_more_rows_and_other_shapes():
+    assert norm_fwd(rows=(1 << 30) + 1) == INVALID and norm_bwd(rows=(1 << 30) + 1, ws_bytes=1 << 40) == INVALID
+    assert lib.als_k_norm_bwd_ws_bytes((1 << 30) + 1, 8) == 0
+    x, g = torch.zeros(2, 3, 4), torch.zeros(4)
+    for call in (lambda: A.k_norm_fwd(x, g), lambda: A.k_norm_fwd(x[0], g, norm="batch"), lambda: A.k_norm_bwd(x, x, g, g, x, g, None),
+                 lambda: A.k_norm_bwd(x[0], x, g, g, x, g, None, norm="batch")):
+        with pytest.raises(A.AlsError):
+            call()
+
+
+def test_one_row_of_any_stride_is_a_matrix():
+    """A single row's stride is never used, so that views of any are taken if the row may be read in pieces of 16 bytes."""
+    buf = torch.zeros(4096, dtype=torch.uint8)
+    ld, data = 100, buf[:1024].view(torch.float8_e4m3fn)
+    one = torch.as_strided(data, (1, 40), (ld, 1))
+    from paper_2401_09135_amd.binding import _rows_of
+    assert _rows_of("x", one, 16)[1] == 48
+    with pytest.raises(A.AlsError):
+        _rows_of("x", torch.as_strided(data, (2, 40), (ld, 1)), 16)
+    with pytest.raises(A.AlsError):
+        _rows_of("x", torch.as_strided(data, (1, 40), (ld, 1), 4096 - 40), 16)

@@ -222,6 +222,25 @@ def test_norm_gradient_against_differences(norm):
         assert abs(num - got) <= 40 * U * size + 1e-9 * size
 
 
+def test_norm_of_more_rows_than_a_launch_has():
+    """The last rows, which a second launch has, and the first: as in a call of their own."""
+    rows, d = (1 << 21) + 37, 24
+    x = torch.randn(rows, d, device=DEV, generator=torch.Generator(DEV).manual_seed(1)).bfloat16()
+    r, gain = torch.randn(rows, d, device=DEV, generator=torch.Generator(DEV).manual_seed(2)), torch.rand(d, device=DEV)
+
+    def run(x, r):
+        n = len(x)
+        out = dict(total=torch.empty(n, d, device=DEV), y=torch.empty(n, d, dtype=torch.bfloat16, device=DEV), rstd=torch.empty(n, device=DEV))
+        q = A.Fp8.empty(n, d)
+        A.k_norm_fwd(x, gain, resid=r, q=q, norm="layer", **out)
+        return [out["total"], out["y"], out["rstd"], q.data.view(torch.uint8), q.scale.view(torch.uint8)]
+
+    every = run(x, r)
+    for at in (0, (1 << 21) - 100, rows - 300):
+        for a, b in zip(every, run(x[at:at + 300].contiguous(), r[at:at + 300].contiguous())):
+            assert torch.equal(a[at:at + 300], b)
+
+
 def test_norm_passes_on_what_is_not_finite():
     x, r, gain = norm_case(8, 300, "f32", 0)
     x[2, 5], x[4, 7] = float("inf"), float("nan")
