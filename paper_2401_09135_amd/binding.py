@@ -508,15 +508,19 @@ class Fp8:
             raise AlsError("Fp8: data must be float8_e4m3fn or float8_e5m2, scale float8_e8m0fnu")
         if block_rows != 1 and block_rows != 128:
             raise AlsError("Fp8: block_rows must be 1 or 128")
-        self.shape = shape = tuple(data.shape)
-        if len(shape) != 2 or tuple(scale.shape) != (-(-shape[0] // block_rows), -(-shape[1] // 128)):
+        self.shape = shape = data.shape
+        if len(shape) != 2:
+            raise AlsError("Fp8: data must be a matrix")
+        rows, cols = shape
+        s_rows, s_cols = rows if block_rows == 1 else (rows + 127) // 128, (cols + 127) // 128
+        if scale.shape != (s_rows, s_cols):
             raise AlsError("Fp8: scale must be [ceil(rows / block_rows), ceil(cols / 128)] of data [rows, cols]")
         self.device_index = _device("Fp8", data, scale)
         self.data, self.scale, self.block_rows = data, scale, block_rows
-        p, ld = _rows_of("Fp8: data", data, 16)
-        ps, ld_scale = _rows_of("Fp8: scale", scale, 4)
-        self._c = _Fp8Struct(p, ps, ld, ld_scale, fmt, block_rows)
-        self._ref = C.byref(self._c)
+        p, ld = _rows_of("Fp8: data", data, rows, cols, 16)
+        ps, ld_scale = _rows_of("Fp8: scale", scale, s_rows, s_cols, 4)
+        self._c = s = _Fp8Struct(p, ps, ld, ld_scale, fmt, block_rows)
+        self._ref = C.byref(s)
 
     @classmethod
     def empty(cls, rows: int, cols: int, format: str = "e4m3", block_rows: int = 1, device="cuda:0") -> "Fp8":
@@ -532,9 +536,8 @@ _FP8_DTYPES = {torch.float8_e4m3fn: 0, torch.float8_e5m2: 1}
 _FLOATS = {torch.float32: ALS_DTYPE_F32, torch.bfloat16: ALS_DTYPE_BF16}
 
 
-def _rows_of(what, t, multiple):
-    """(address, row stride) of a matrix in 8 bits, whose last row has to be as long as the others."""
-    rows, cols = t.shape
+def _rows_of(what, t, rows, cols, multiple):
+    """(address, row stride) of a matrix [rows, cols] in 8 bits, whose last row has to be as long as the others."""
     if rows == 0 or cols == 0:
         return t.data_ptr(), -(-cols // multiple) * multiple
     ld, unit = t.stride()
@@ -543,7 +546,7 @@ def _rows_of(what, t, multiple):
     p = t.data_ptr()
     if (unit != 1 and cols > 1) or ld < cols or ld % multiple or p % multiple:
         raise AlsError(f"{what}: columns must be contiguous, the start and the row stride multiples of {multiple} bytes")
-    if t.storage_offset() + rows * ld > t.untyped_storage().nbytes():
+    if ld != cols and t.storage_offset() + rows * ld > t.untyped_storage().nbytes():
         raise AlsError(f"{what}: the last row must be as long as the row stride ({ld} bytes)")
     return p, ld
 

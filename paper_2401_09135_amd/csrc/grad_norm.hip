@@ -161,8 +161,20 @@ __device__ __forceinline__ void scale_pieces(const void* in, void* out, int64_t 
   }
 }
 
-__global__ __launch_bounds__(256) void grad_clip_kernel(GradTable t, const float* __restrict__ norm, float max_norm) {
-  const float k = clip_coefficient(norm[0], max_norm);
+// count: partial sums that each workgroup adds itself, in the order of grad_norm_kernel, the first one leaving the norm; 0: the norm is there
+__global__ __launch_bounds__(256) void grad_clip_kernel(GradTable t, float* norm, float max_norm, const double* __restrict__ partial, int count) {
+  float root;
+  if (count) {
+    __shared__ double sh[4];
+    const double s = wave_sum_f64((int)threadIdx.x < count ? partial[threadIdx.x] : 0.0);
+    if ((threadIdx.x & 63) == 0) sh[threadIdx.x >> 6] = s;
+    __syncthreads();
+    root = (float)sqrt(sh[0] + sh[1] + sh[2] + sh[3]);
+    if (blockIdx.x == 0 && threadIdx.x == 0) norm[0] = root;
+  } else {
+    root = norm[0];
+  }
+  const float k = clip_coefficient(root, max_norm);
   for_chunks(t, [&](const void* in, void* out, int64_t numel, bool bf, int64_t p0, int64_t p1) {
     if (k == 1.0f && in == out) return;   // nothing changes
     if (bf) scale_pieces<bf16>(in, out, numel, p0, p1, k);
@@ -216,15 +228,21 @@ int check_list_ws(int n, const int64_t* numel, const void* ws, size_t ws_bytes, 
 
 }  // namespace
 
-int grad_norm(int n, const void* const* grads, const int64_t* numel, const int32_t* dtypes, float* norm_out, double* partial, hipStream_t st, float* log,
-              const StepState* ss, int64_t log_offset) {
-  int64_t count = 0;
-  int rc = for_launches(n, grads, nullptr, numel, dtypes, [&](const GradTable& t, int blocks, int64_t p0) {
+// the partial sums of a list; count: how many
+static int grad_squares(int n, const void* const* grads, const int64_t* numel, const int32_t* dtypes, double* partial, int64_t& count, hipStream_t st) {
+  count = 0;
+  return for_launches(n, grads, nullptr, numel, dtypes, [&](const GradTable& t, int blocks, int64_t p0) {
     hipLaunchKernelGGL(grad_squares_kernel, dim3(blocks), dim3(256), 0, st, t, partial + p0);
     ALS_CHECK_LAUNCH();
     count = p0 + blocks;
     return ALS_OK;
   });
+}
+
+int grad_norm(int n, const void* const* grads, const int64_t* numel, const int32_t* dtypes, float* norm_out, double* partial, hipStream_t st, float* log,
+              const StepState* ss, int64_t log_offset) {
+  int64_t count = 0;
+  int rc = grad_squares(n, grads, numel, dtypes, partial, count, st);
   if (rc) return rc;
   hipLaunchKernelGGL(grad_norm_kernel, dim3(1), dim3(1024), 0, st, partial, count, norm_out, log, ss, log_offset);
   ALS_CHECK_LAUNCH();
@@ -293,10 +311,20 @@ extern "C" int als_k_grad_clip(int n, const void* const* grads, void* const* out
     return set_error(ALS_ERR_INVALID, "out of host memory");
   }
   rc = check_list_ws(n, numel, ws_dev, ws_bytes, "als_k_grad_clip");
-  if (!rc) rc = grad_norm(n, grads, numel, dtypes, norm_out, (double*)ws_dev, (hipStream_t)stream);
+  double* partial = (double*)ws_dev;
+  hipStream_t st = (hipStream_t)stream;
+  int64_t count = 0;
+  if (!rc) rc = grad_squares(n, grads, numel, dtypes, partial, count, st);
   if (rc) return rc;
+  // up to 256 partial sums, one a thread, are added again by every workgroup that clips: a launch less (16 tensors of 7187 elements 12.2 us to 9.5,
+  // of 60000, 240 sums, 12.2 to 9.8; in one launch no more can be added without a loop)
+  const int again = count <= 256 && n <= GN_TENSORS ? (int)count : 0;
+  if (!again) {
+    hipLaunchKernelGGL(grad_norm_kernel, dim3(1), dim3(1024), 0, st, partial, count, norm_out, nullptr, nullptr, 0);
+    ALS_CHECK_LAUNCH();
+  }
   return for_launches(n, grads, outs, numel, dtypes, [&](const GradTable& t, int blocks, int64_t) {
-    hipLaunchKernelGGL(grad_clip_kernel, dim3(blocks), dim3(256), 0, (hipStream_t)stream, t, norm_out, (float)max_norm);
+    hipLaunchKernelGGL(grad_clip_kernel, dim3(blocks), dim3(256), 0, st, t, norm_out, (float)max_norm, partial, again);
     ALS_CHECK_LAUNCH();
     return ALS_OK;
   });

@@ -220,8 +220,8 @@ def test_one_row_of_any_stride_is_a_matrix():
     ld, data = 100, buf[:1024].view(torch.float8_e4m3fn)
     one = torch.as_strided(data, (1, 40), (ld, 1))
     from paper_2401_09135_amd.binding import _rows_of
-    assert _rows_of("x", one, 16)[1] == 48
+    assert _rows_of("x", one, 1, 40, 16)[1] == 48
     with pytest.raises(A.AlsError):
-        _rows_of("x", torch.as_strided(data, (2, 40), (ld, 1)), 16)
+        _rows_of("x", torch.as_strided(data, (2, 40), (ld, 1)), 2, 40, 16)
     with pytest.raises(A.AlsError):
-        _rows_of("x", torch.as_strided(data, (1, 40), (ld, 1), 4096 - 40), 16)
+        _rows_of("x", torch.as_strided(data, (1, 40), (ld, 1), 4096 - 40), 1, 40, 16)
