@@ -26,6 +26,12 @@ __device__ __forceinline__ unsigned lanes16_max(unsigned m) {
 #undef ALS_DPP_MAX
   return m;
 }
+// the largest of 32
+__device__ __forceinline__ unsigned lanes32_max(unsigned m) {
+  m = lanes16_max(m);
+  auto a = __builtin_amdgcn_permlane16_swap(m, m, false, false);
+  return a[0] > a[1] ? a[0] : a[1];
+}
 // bits of |v|, 0 for what is not finite
 __device__ __forceinline__ unsigned fp8_magnitude(float v) {
   const unsigned u = __builtin_bit_cast(unsigned, v) & 0x7fffffffu;
@@ -45,50 +51,41 @@ __device__ __forceinline__ unsigned fp8_pack4(float a, float b, float c, float d
   return __builtin_bit_cast(unsigned, v);
 }
 
-// Eight consecutive elements from p, at any address of their type (the memory takes 16 bytes anywhere); elements from n on are 0 and not read.
-__device__ __forceinline__ void load8(const float* p, int n, float (&v)[8]) {
-  if (n >= 8) {
-    __builtin_memcpy(v, p, 32);
-  } else {
-#pragma unroll
-    for (int i = 0; i < 8; i++) v[i] = i < n ? p[i] : 0.0f;
-  }
-}
-__device__ __forceinline__ void load8(const bf16* p, int n, float (&v)[8]) {
-  if (n >= 8) {
-    bf16x8 a;
-    __builtin_memcpy(&a, p, 16);
-#pragma unroll
-    for (int i = 0; i < 8; i++) v[i] = (float)a[i];
-  } else {
-#pragma unroll
-    for (int i = 0; i < 8; i++) v[i] = i < n ? (float)p[i] : 0.0f;
-  }
-}
-// Non-temporal: what a pass over memory writes is no use in the caches that hold what it reads (norms of 16384 x 896: forward 48 us to 43.5, backward 52 to 48.5; quantiser
-// of 16384 x 3584 bf16 in both orientations 55.5 to 51.5; loads gain nothing).
+// Non-temporal: what a pass over memory writes is no use in the caches that hold what it reads (quantiser of 16384 x 3584 bf16 in both
+// orientations 55.5 to 51.5 us, norms 7 to 10 %; loads gain nothing).
 typedef float f32x4_any __attribute__((ext_vector_type(4), aligned(4)));
-typedef unsigned u32x4_any __attribute__((ext_vector_type(4), aligned(2)));
-__device__ __forceinline__ void store8(float* p, int n, const float (&v)[8]) {
-  if (n >= 8) {
+typedef unsigned u32x2_any __attribute__((ext_vector_type(2), aligned(2)));
+// Four consecutive elements to p, at any address of their type; only the first n.
+__device__ __forceinline__ void store4(float* p, int n, const float (&v)[4]) {
+  if (n >= 4) {
     __builtin_nontemporal_store((f32x4_any){v[0], v[1], v[2], v[3]}, reinterpret_cast<f32x4_any*>(p));
-    __builtin_nontemporal_store((f32x4_any){v[4], v[5], v[6], v[7]}, reinterpret_cast<f32x4_any*>(p) + 1);
   } else {
 #pragma unroll
-    for (int i = 0; i < 8; i++)
+    for (int i = 0; i < 4; i++)
       if (i < n) p[i] = v[i];
   }
 }
-__device__ __forceinline__ void store8(bf16* p, int n, const float (&v)[8]) {
-  if (n >= 8) {
-    bf16x8 a;
+__device__ __forceinline__ void store4(bf16* p, int n, const float (&v)[4]) {
+  typedef unsigned u32x2 __attribute__((ext_vector_type(2)));
+  if (n >= 4) {
+    bf16x4 a;
 #pragma unroll
-    for (int i = 0; i < 8; i++) a[i] = (bf16)v[i];
-    __builtin_nontemporal_store((u32x4_any)__builtin_bit_cast(u32x4, a), reinterpret_cast<u32x4_any*>(p));
+    for (int i = 0; i < 4; i++) a[i] = (bf16)v[i];
+    __builtin_nontemporal_store((u32x2_any)__builtin_bit_cast(u32x2, a), reinterpret_cast<u32x2_any*>(p));
   } else {
 #pragma unroll
-    for (int i = 0; i < 8; i++)
+    for (int i = 0; i < 4; i++)
       if (i < n) p[i] = (bf16)v[i];
+  }
+}
+// four bytes to p, which is 4-byte aligned; only the first n of them
+__device__ __forceinline__ void store4_bytes(uint8_t* p, int n, unsigned v) {
+  if (n >= 4) {
+    __builtin_nontemporal_store(v, reinterpret_cast<unsigned*>(p));
+  } else {
+#pragma unroll
+    for (int i = 0; i < 4; i++)
+      if (i < n) p[i] = (uint8_t)(v >> (8 * i));
   }
 }
 // eight bytes to p, which is 8-byte aligned; only the first n of them

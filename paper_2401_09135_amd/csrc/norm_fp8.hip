@@ -1,8 +1,13 @@
 // Norm with the residual's addition and an output in 8 bits (als_k_norm_fwd), and its backward pass (als_k_norm_bwd), for rows of up to 16384 elements.
 //
-// Memory bounds both: every tensor is read or written once.  A row stays in the registers of a wavefront (d <= 1024), of 256 threads (d <= 4096) or of
-// 1024; a thread has up to 2 runs of 8 consecutive elements of it, so that a block of 128 is 16 neighbouring lanes' and its scale needs no LDS.
+// Memory bounds both: every tensor is read or written once.  A row stays in the registers of a wavefront (d <= 1024), of 256 threads (d <= 4096) or of 1024; a thread
+// has 2 or 4 runs of 4 consecutive elements of it, so that a load or store of fp32 is 1 KB without gaps for a wavefront, and a block of 128 is 32 neighbouring lanes', whose
+// scale needs no LDS.  The backward pass loads a row while it works on the one before.  16384 x 896, forward (fp32 input, all outputs) 39.4 us, 5.6 TB/s; backward (bf16 dy, all
+// outputs) 46.5 us, 5.05 TB/s with the second launch that adds the gain's gradient.  With runs of 8, loaded behind branches, and no row ahead: 43 and 49.5; 16384 x 1023 backward
+// 57 and 70; 16384 x 512 backward 25.4 and 28.5; 1000 x 16000 backward 83 and 85; with 4 runs where 2 reach 16384 x 512 backward 28, 2000 x 8192 forward 56 instead of 46.
 #include "fp8.h"
+
+#include <type_traits>
 
 namespace als {
 
@@ -30,7 +35,51 @@ __device__ __forceinline__ float row_sum(float v, float* sh) {
   return s;
 }
 
-constexpr int NORM_RUNS = 2;   // runs of 8 elements of a thread
+// Element c of a row whose address all lanes share, by a 32-bit offset: a register a lane instead of two
+template <typename P>
+__device__ __forceinline__ P* element(P* row, int c) {
+  typedef typename std::conditional<std::is_const<P>::value, const char, char>::type byte;
+  return reinterpret_cast<P*>(reinterpret_cast<byte*>(row) + (unsigned)c * (unsigned)sizeof(P));
+}
+
+// A thread's elements of a row as they lie in memory, runs of 4, run s at 4 (t + NT s).  What is loaded is not used, and so not waited for, before settle() and
+// at(), and loads have no branches: a run that the row ends in or before is the row's last 4 elements in its place.
+template <typename T, int NT, int RUNS>
+struct RowPart {
+  typedef T run __attribute__((ext_vector_type(4)));
+  run v[RUNS];
+  __device__ __forceinline__ void load(const T* row, int d, int t) {
+    if (d >= 4) {
+#pragma unroll
+      for (int s = 0; s < RUNS; s++) {
+        const int c = 4 * (t + NT * s);
+        __builtin_memcpy(&v[s], element(row, c < d - 4 ? c : d - 4), sizeof(run));
+      }
+    } else {
+#pragma unroll
+      for (int i = 0; i < 3; i++) v[0][i] = row[i < d ? i : 0];
+    }
+  }
+  // moves the elements of a run that the row ends in to their places
+  __device__ __forceinline__ void settle(int d, int t) {
+    if (d % 4 == 0) return;
+    const T z = (T)0.0f;
+    if (d < 4) {
+      if (d < 3) v[0][2] = z;
+      if (d < 2) v[0][1] = z;
+      v[0][3] = z;
+      return;
+    }
+#pragma unroll
+    for (int s = 0; s < RUNS; s++) {
+      const int k = 4 * (t + NT * s) - (d - 4);   // 1, 2 or 3 in such a run
+      const run x = v[s];
+      v[s] = k == 1 ? (run){x[1], x[2], x[3], z} : k == 2 ? (run){x[2], x[3], z, z} : k == 3 ? (run){x[3], z, z, z} : x;
+    }
+  }
+  // 0 outside the row
+  __device__ __forceinline__ float at(int s, int i, int d, int t) const { return 4 * (t + NT * s) < d ? (float)v[s][i] : 0.0f; }
+};
 
 struct NormFwdArgs {
   const void* x; const float* resid; const float* gain; float* total; bf16* y;
@@ -39,72 +88,77 @@ struct NormFwdArgs {
 };
 
 // NT threads a row; NT = 64: four rows a workgroup
-template <typename T, int NT, bool CENTER>
+template <typename T, int NT, int RUNS, bool CENTER>
 __global__ __launch_bounds__(NT == 64 ? 256 : NT) void norm_fwd_kernel(NormFwdArgs a) {
   __shared__ float sh[NT / 64];
   const int t = NT == 64 ? threadIdx.x & 63 : threadIdx.x;
-  const int row = NT == 64 ? blockIdx.x * 4 + (threadIdx.x >> 6) : blockIdx.x;
+  const int row = NT == 64 ? blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6) : blockIdx.x;
   if (row >= a.rows) return;   // a whole wavefront, or nobody where the threads of a row meet
   const int64_t base = (int64_t)row * a.d;
-  float v[NORM_RUNS][8], e[NORM_RUNS][8];
+  RowPart<T, NT, RUNS> x;
+  RowPart<float, NT, RUNS> resid, gain;
+  x.load((const T*)a.x + base, a.d, t);
+  if (a.resid) resid.load(a.resid + base, a.d, t);
+  gain.load(a.gain, a.d, t);
+  x.settle(a.d, t);
+  float v[RUNS][4];
   float sum = 0.0f;
 #pragma unroll
-  for (int s = 0; s < NORM_RUNS; s++) load8((const T*)a.x + base + 8 * (t + NT * s), a.d - 8 * (t + NT * s), v[s]);
+  for (int s = 0; s < RUNS; s++)
+#pragma unroll
+    for (int i = 0; i < 4; i++) v[s][i] = x.at(s, i, a.d, t);
   if (a.resid) {
+    resid.settle(a.d, t);
 #pragma unroll
-    for (int s = 0; s < NORM_RUNS; s++) load8(a.resid + base + 8 * (t + NT * s), a.d - 8 * (t + NT * s), e[s]);
+    for (int s = 0; s < RUNS; s++) {
 #pragma unroll
-    for (int s = 0; s < NORM_RUNS; s++) {
-#pragma unroll
-      for (int i = 0; i < 8; i++) v[s][i] += e[s][i];
-      store8(a.total + base + 8 * (t + NT * s), a.d - 8 * (t + NT * s), v[s]);
+      for (int i = 0; i < 4; i++) v[s][i] += resid.at(s, i, a.d, t);
+      store4(element(a.total + base, 4 * (t + NT * s)), a.d - 4 * (t + NT * s), v[s]);
     }
   }
-#pragma unroll
-  for (int s = 0; s < NORM_RUNS; s++) load8(a.gain + 8 * (t + NT * s), a.d - 8 * (t + NT * s), e[s]);
   if (CENTER)
 #pragma unroll
-    for (int s = 0; s < NORM_RUNS; s++)
+    for (int s = 0; s < RUNS; s++)
 #pragma unroll
-      for (int i = 0; i < 8; i++) sum += v[s][i];
+      for (int i = 0; i < 4; i++) sum += v[s][i];
   if (CENTER) {
     const float mean = row_sum<NT>(sum, sh) / (float)a.d;
 #pragma unroll
-    for (int s = 0; s < NORM_RUNS; s++)
+    for (int s = 0; s < RUNS; s++)
 #pragma unroll
-      for (int i = 0; i < 8; i++)
-        if (8 * (t + NT * s) + i < a.d) v[s][i] -= mean;
+      for (int i = 0; i < 4; i++)
+        if (4 * (t + NT * s) + i < a.d) v[s][i] -= mean;
   }
   float ss = 0.0f;
 #pragma unroll
-  for (int s = 0; s < NORM_RUNS; s++)
+  for (int s = 0; s < RUNS; s++)
 #pragma unroll
-    for (int i = 0; i < 8; i++) ss += v[s][i] * v[s][i];
+    for (int i = 0; i < 4; i++) ss += v[s][i] * v[s][i];
   ss = row_sum<NT>(ss, sh);
   // rstd in two parts, and each product with what its rounding left: an output in 8 bits turns an error of one rounding into a step of 1/16 where it falls on a border,
-  // and what follows is rounded once.  (0.5 us of 48.)
+  // and what follows is rounded once.  (0.5 us of 40.)
+  gain.settle(a.d, t);
   const double rd = 1.0 / sqrt((double)ss / a.d + (double)a.eps);
   const float r = (float)rd, r_rest = (float)(rd - (double)r);
   if (t == 0) a.rstd[row] = r;
 #pragma unroll
-  for (int s = 0; s < NORM_RUNS; s++) {
-    const int c = 8 * (t + NT * s), n = a.d - c;
+  for (int s = 0; s < RUNS; s++) {
+    const int c = 4 * (t + NT * s), n = a.d - c;
 #pragma unroll
-    for (int i = 0; i < 8; i++) {
-      const float p = v[s][i] * e[s][i], p_rest = fmaf(v[s][i], e[s][i], -p);
+    for (int i = 0; i < 4; i++) {
+      const float e = gain.at(s, i, a.d, t), p = v[s][i] * e, p_rest = fmaf(v[s][i], e, -p);
       v[s][i] = fmaf(p, r, fmaf(p, r_rest, p_rest * r));
     }
-    if (a.y) store8(a.y + base + c, n, v[s]);
+    if (a.y) store4(element(a.y + base, c), n, v[s]);
     if (a.q) {
       unsigned m = 0;
 #pragma unroll
-      for (int i = 0; i < 8; i++) m = max(m, fp8_magnitude(v[s][i]));
-      const int b = fp8_scale_byte(lanes16_max(m), a.format);
+      for (int i = 0; i < 4; i++) m = max(m, fp8_magnitude(v[s][i]));
+      const int b = fp8_scale_byte(lanes32_max(m), a.format);
       const float sc = fp8_scale(b);
       if (n > 0) {
-        if ((t & 15) == 0) a.scale[(int64_t)row * a.ld_scale + c / 128] = (uint8_t)b;
-        store8_bytes(a.q + (int64_t)row * a.ld + c, n, fp8_pack4(v[s][0], v[s][1], v[s][2], v[s][3], sc, a.format),
-                     fp8_pack4(v[s][4], v[s][5], v[s][6], v[s][7], sc, a.format));
+        if ((t & 31) == 0) a.scale[(int64_t)row * a.ld_scale + c / 128] = (uint8_t)b;
+        store4_bytes(element(a.q + (int64_t)row * a.ld, c), n, fp8_pack4(v[s][0], v[s][1], v[s][2], v[s][3], sc, a.format));
       }
     }
   }
@@ -122,83 +176,124 @@ int norm_bwd_blocks(int rows, int d) {
   return b < 512 ? b : 512;
 }
 
-template <typename T, int NT, bool CENTER>
+template <typename T, int NT, int RUNS, bool CENTER>
 __global__ __launch_bounds__(NT == 64 ? 256 : NT) void norm_bwd_kernel(NormBwdArgs a) {
   constexpr int AT_ONCE = NT == 64 ? 4 : 1;
   __shared__ float sh[NT / 64];
   __shared__ float parts[NT == 64 ? 3 : 1][NT == 64 ? 1024 : 1];
-  const int t = NT == 64 ? threadIdx.x & 63 : threadIdx.x, w = NT == 64 ? threadIdx.x >> 6 : 0;
+  const int t = NT == 64 ? threadIdx.x & 63 : threadIdx.x, w = NT == 64 ? __builtin_amdgcn_readfirstlane(threadIdx.x >> 6) : 0;
   const float inv_d = 1.0f / (float)a.d;
-  float dg[NORM_RUNS][8], g[NORM_RUNS][8];
-#pragma unroll
-  for (int s = 0; s < NORM_RUNS; s++) {
-    load8(a.gain + 8 * (t + NT * s), a.d - 8 * (t + NT * s), g[s]);
-#pragma unroll
-    for (int i = 0; i < 8; i++) dg[s][i] = 0.0f;
-  }
-  for (int row = blockIdx.x * AT_ONCE + w; row < a.rows; row += gridDim.x * AT_ONCE) {
+  float dg[RUNS][4];
+  // The next row is loaded while one is worked on.  1024 threads with 4 runs have 128 registers each and no room for that; their gain and its gradient are in LDS (with all in
+  // registers, some of them in scratch memory, 1000 rows of 16000 take 148 us).
+  constexpr bool AHEAD = NT * RUNS <= 2048;
+  __shared__ f32x4 kept[2][AHEAD ? 1 : RUNS][AHEAD ? 1 : NT];
+  RowPart<float, NT, RUNS> gain, total, in;
+  RowPart<T, NT, RUNS> dy;
+  float rstd = 0.0f;
+  auto load = [&](int row) {
+    if (row >= a.rows) return;
     const int64_t base = (int64_t)row * a.d;
-    const float r = a.rstd[row];
-    float x[NORM_RUNS][8], h[NORM_RUNS][8];
+    rstd = a.rstd[row];
+    total.load(a.total + base, a.d, t);
+    dy.load((const T*)a.dy + base, a.d, t);
+    if (AHEAD && a.ds_in) in.load(a.ds_in + base, a.d, t);
+  };
+  gain.load(a.gain, a.d, t);
+  const int stride = gridDim.x * AT_ONCE;
+  int row = blockIdx.x * AT_ONCE + w;
+  if (AHEAD) load(row);
+  gain.settle(a.d, t);
+#pragma unroll
+  for (int s = 0; s < RUNS; s++) {
+#pragma unroll
+    for (int i = 0; i < 4; i++) dg[s][i] = 0.0f;
+    if (!AHEAD) {
+      kept[0][s][t] = gain.v[s];
+      kept[1][s][t] = (f32x4){0.0f, 0.0f, 0.0f, 0.0f};
+    }
+  }
+  for (; row < a.rows; row += stride) {
+    const int64_t base = (int64_t)row * a.d;
+    int d = a.d;
+    asm volatile("" : "+s"(d));   // comparisons with it are made in every row: two registers each to keep them for all rows are too many
+    if (!AHEAD) load(row);
+    total.settle(d, t);
+    dy.settle(d, t);
+    const float r = rstd;
+    float x[RUNS][4], h[RUNS][4];
     float sx = 0.0f, sh1 = 0.0f, dot = 0.0f;
 #pragma unroll
-    for (int s = 0; s < NORM_RUNS; s++) {
-      const int c = 8 * (t + NT * s), n = a.d - c;
-      load8(a.total + base + c, n, x[s]);
-      load8((const T*)a.dy + base + c, n, h[s]);
-      if (CENTER)
+    for (int s = 0; s < RUNS; s++)
 #pragma unroll
-        for (int i = 0; i < 8; i++) sx += x[s][i];
-    }
+      for (int i = 0; i < 4; i++) {
+        x[s][i] = total.at(s, i, d, t);
+        h[s][i] = dy.at(s, i, d, t);
+        if (CENTER) sx += x[s][i];
+      }
+    RowPart<float, NT, RUNS> add = in;
+    if (AHEAD) load(row + stride);
     const float mean = CENTER ? row_sum<NT>(sx, sh) * inv_d : 0.0f;
 #pragma unroll
-    for (int s = 0; s < NORM_RUNS; s++)
+    for (int s = 0; s < RUNS; s++) {
+      if (!AHEAD) gain.v[s] = kept[0][s][t];
+      f32x4 sum = AHEAD ? (f32x4){dg[s][0], dg[s][1], dg[s][2], dg[s][3]} : kept[1][s][t];
 #pragma unroll
-      for (int i = 0; i < 8; i++) {
-        const bool in = 8 * (t + NT * s) + i < a.d;
-        x[s][i] = CENTER ? (in ? (x[s][i] - mean) * r : 0.0f) : x[s][i] * r;   // xh
-        dg[s][i] += h[s][i] * x[s][i];
-        h[s][i] *= g[s][i];
+      for (int i = 0; i < 4; i++) {
+        x[s][i] = (CENTER ? x[s][i] - mean : x[s][i]) * r;   // xh; outside the row h is 0
+        sum[i] += h[s][i] * x[s][i];
+        h[s][i] *= gain.at(s, i, d, t);
         sh1 += h[s][i];
         dot += h[s][i] * x[s][i];
+        if (AHEAD) dg[s][i] = sum[i];
       }
+      if (!AHEAD) kept[1][s][t] = sum;
+    }
     dot = row_sum<NT>(dot, sh) * inv_d;
     const float m1 = CENTER ? row_sum<NT>(sh1, sh) * inv_d : 0.0f;
 #pragma unroll
-    for (int s = 0; s < NORM_RUNS; s++) {
-      const int c = 8 * (t + NT * s), n = a.d - c;
-      float o[8];
+    for (int s = 0; s < RUNS; s++) {
 #pragma unroll
-      for (int i = 0; i < 8; i++) o[i] = r * (h[s][i] - m1 - x[s][i] * dot);
-      if (a.ds_in) {
-        float in[8];
-        load8(a.ds_in + base + c, n, in);
-#pragma unroll
-        for (int i = 0; i < 8; i++) o[i] += in[i];
-      }
-      store8(a.ds + base + c, n, o);
-      if (a.lp) store8(a.lp + base + c, n, o);
+      for (int i = 0; i < 4; i++) h[s][i] = r * (h[s][i] - m1 - x[s][i] * dot);
     }
+    if (a.ds_in) {
+      if (!AHEAD) add.load(a.ds_in + base, d, t);
+      add.settle(d, t);
+#pragma unroll
+      for (int s = 0; s < RUNS; s++)
+#pragma unroll
+        for (int i = 0; i < 4; i++) h[s][i] += (float)add.v[s][i];
+    }
+#pragma unroll
+    for (int s = 0; s < RUNS; s++) {
+      const int c = 4 * (t + NT * s);
+      store4(element(a.ds + base, c), d - c, h[s]);
+      if (a.lp) store4(element(a.lp + base, c), d - c, h[s]);
+    }
+  }
+  if (!AHEAD) {
+#pragma unroll
+    for (int s = 0; s < RUNS; s++) __builtin_memcpy(dg[s], &kept[1][s][t], 16);
   }
   float* out = a.partial + (int64_t)blockIdx.x * a.d;
   if (NT == 64) {   // the four wavefronts' sums, in their order
     if (w)
 #pragma unroll
-      for (int s = 0; s < NORM_RUNS; s++) __builtin_memcpy(parts[w - 1] + 8 * (t + NT * s), dg[s], 32);
+      for (int s = 0; s < RUNS; s++) __builtin_memcpy(parts[w - 1] + 4 * (t + NT * s), dg[s], 16);
     __syncthreads();
     if (w) return;
 #pragma unroll
-    for (int s = 0; s < NORM_RUNS; s++)
+    for (int s = 0; s < RUNS; s++)
 #pragma unroll
       for (int j = 0; j < 3; j++) {
-        float o[8];
-        load8(parts[j] + 8 * (t + NT * s), 8, o);
+        float o[4];
+        __builtin_memcpy(o, parts[j] + 4 * (t + NT * s), 16);
 #pragma unroll
-        for (int i = 0; i < 8; i++) dg[s][i] += o[i];
+        for (int i = 0; i < 4; i++) dg[s][i] += o[i];
       }
   }
 #pragma unroll
-  for (int s = 0; s < NORM_RUNS; s++) store8(out + 8 * (t + NT * s), a.d - 8 * (t + NT * s), dg[s]);
+  for (int s = 0; s < RUNS; s++) store4(element(out, 4 * (t + NT * s)), a.d - 4 * (t + NT * s), dg[s]);
 }
 
 // dgain = the sum of the blocks' rows, in the order of the blocks: 16 columns a workgroup, 64 groups of lanes each with every 64th row
@@ -232,18 +327,21 @@ __global__ __launch_bounds__(1024) void norm_dgain_kernel(const float* __restric
 
 using namespace als;
 
-// Launches KERNEL<T, NT, CENTER> for a row of d
-#define ALS_NORM_C(KERNEL, T, NT, GRID) \
+// Launches KERNEL<T, NT, RUNS, CENTER> for a row of d: as few threads as hold it, in half as many runs where those reach
+#define ALS_NORM_C(KERNEL, T, NT, RUNS, GRID) \
   do { \
     const dim3 grid_(GRID), block_(NT == 64 ? 256 : NT); \
-    if (center) hipLaunchKernelGGL((KERNEL<T, NT, true>), grid_, block_, 0, st, a); \
-    else hipLaunchKernelGGL((KERNEL<T, NT, false>), grid_, block_, 0, st, a); \
+    if (center) hipLaunchKernelGGL((KERNEL<T, NT, RUNS, true>), grid_, block_, 0, st, a); \
+    else hipLaunchKernelGGL((KERNEL<T, NT, RUNS, false>), grid_, block_, 0, st, a); \
   } while (0)
 #define ALS_NORM(KERNEL, T, GRID64, GRID) \
   do { \
-    if (d <= 1024) ALS_NORM_C(KERNEL, T, 64, GRID64); \
-    else if (d <= 4096) ALS_NORM_C(KERNEL, T, 256, GRID); \
-    else ALS_NORM_C(KERNEL, T, 1024, GRID); \
+    if (d <= 512) ALS_NORM_C(KERNEL, T, 64, 2, GRID64); \
+    else if (d <= 1024) ALS_NORM_C(KERNEL, T, 64, 4, GRID64); \
+    else if (d <= 2048) ALS_NORM_C(KERNEL, T, 256, 2, GRID); \
+    else if (d <= 4096) ALS_NORM_C(KERNEL, T, 256, 4, GRID); \
+    else if (d <= 8192) ALS_NORM_C(KERNEL, T, 1024, 2, GRID); \
+    else ALS_NORM_C(KERNEL, T, 1024, 4, GRID); \
   } while (0)
 
 static int check_norm(int rows, int d, int norm_kind, const char* what) {

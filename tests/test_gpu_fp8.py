@@ -126,7 +126,11 @@ def norm_case(rows, d, dtype, seed, zeros=True):
     return x, r, gain
 
 
-@pytest.mark.parametrize("rows,d", NORM_SIZES)
+# on either side of where the kernels change, and rows that end in each place of a run
+NORM_BORDERS = [(5, d) for d in (2, 4, 5, 6, 511, 512, 513, 1022, 1025, 2047, 2048, 2049, 4095, 4098, 8191, 8192, 8193, 12289, 16381, 16383)]
+
+
+@pytest.mark.parametrize("rows,d", NORM_SIZES + NORM_BORDERS)
 @pytest.mark.parametrize("norm", ["rms", "layer"])
 @pytest.mark.parametrize("dtype,add", [("f32", True), ("bf16", True), ("bf16", False), ("f32", False)])
 def test_norm_forward(rows, d, norm, dtype, add):
@@ -168,7 +172,7 @@ def test_norm_forward(rows, d, norm, dtype, add):
         assert torch.equal(r2, total)
 
 
-@pytest.mark.parametrize("rows,d", NORM_SIZES + [(2500, 48), (0, 100)])
+@pytest.mark.parametrize("rows,d", NORM_SIZES + NORM_BORDERS + [(2500, 48), (0, 100), (1200, 9001)])
 @pytest.mark.parametrize("norm", ["rms", "layer"])
 @pytest.mark.parametrize("dtype,add", [("f32", True), ("bf16", True), ("bf16", False)])
 def test_norm_backward(rows, d, norm, dtype, add):
