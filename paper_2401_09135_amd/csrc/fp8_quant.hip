@@ -4,8 +4,9 @@
 // both orientations; a thread has 8 rows of 8 columns of it in registers, so that a row's largest magnitude is 16 neighbouring lanes' and the bytes of
 // a thread are 8 in a row of either orientation.  The transposed bytes go through LDS (16 KB) to be written as whole rows of 128.
 // Magnitudes are compared as whole numbers, two bf16 at a time, and the conversion divides by the scale: 3 vector instructions an element in bf16 and both
-// orientations.  Scales are written as single bytes, which meet their neighbours in an L2: every XCD has a run of neighbouring tiles.
-// 16384 x 3584 bf16, both orientations: 51.5 us with a scale a row, 45.7 with one a tile (5.1 TB/s, a copy of that size 5.4); with magnitudes in floating point,
+// orientations.  Scales are written as single bytes, a tile's rows and columns in one store each (51.5 us otherwise), which meet their neighbours in an L2: every XCD has a run of
+// neighbouring tiles.
+// 16384 x 3584 bf16, both orientations: 50 us with a scale a row, 46.4 with one a tile (5.1 TB/s, a copy of that size 5.4); with magnitudes in floating point,
 // products by 1 / scale, tiles dealt to the XCDs in turn and ordinary stores 70 and 55.  Bands of tiles column by column, for the transposed scales, gain 1 us of 56, but with
 // 4096 columns take 74 instead of 67.
 #include "fp8.h"
@@ -138,6 +139,7 @@ template <typename T, bool Q, bool QT>
 __global__ __launch_bounds__(256) void quant_fp8_kernel(const T* __restrict__ x, int rows, int cols, int64_t ldx, Fp8Out q, Fp8Out qt, int tiles_c) {
   __shared__ __attribute__((aligned(16))) unsigned cmax[QT ? 4 : 1][QT ? 128 : 4];
   __shared__ unsigned wmax[4];
+  __shared__ uint8_t scales[2][128];   // of the tile's rows and columns, written together: a thread each
   __shared__ __attribute__((aligned(16))) uint8_t tile[QT ? 128 * 128 : 16];
   const int total = gridDim.x, base = total / 8, rem = total % 8, xcd = blockIdx.x & 7;
   const int id = xcd * base + (xcd < rem ? xcd : rem) + (blockIdx.x >> 3);
@@ -180,7 +182,7 @@ __global__ __launch_bounds__(256) void quant_fp8_kernel(const T* __restrict__ x,
       int b = bt;
       if (q.block_rows == 1) {
         b = fp8_scale_byte(lanes16_max(rmax[i]), q.format);
-        if (cx == 0 && r0 + i < rows) q.scale[(int64_t)(r0 + i) * q.ld_scale + tc] = (uint8_t)b;
+        if (cx == 0) scales[0][8 * ry + i] = (uint8_t)b;
       }
       const float s = fp8_scale(b);
       const unsigned lo = v.row4(i, 0, s, q.format), hi = v.row4(i, 1, s, q.format);
@@ -207,12 +209,17 @@ __global__ __launch_bounds__(256) void quant_fp8_kernel(const T* __restrict__ x,
       int b = bt;
       if (qt.block_rows == 1) {
         b = fp8_scale_byte(cm[j], qt.format);
-        if (ry == 0 && j < left) qt.scale[(int64_t)(c + j) * qt.ld_scale + tr] = (uint8_t)b;
+        if (ry == 0) scales[1][8 * cx + j] = (uint8_t)b;
       }
       const float s = fp8_scale(b);
       *reinterpret_cast<uint2*>(tile + (8 * cx + j) * 128 + (ry ^ cx) * 8) = make_uint2(v.col4(j, 0, s, qt.format), v.col4(j, 1, s, qt.format));
     }
-    __syncthreads();
+  }
+  if (QT || q.block_rows == 1) __syncthreads();
+  const int line = threadIdx.x & 127;
+  if (Q && q.block_rows == 1 && threadIdx.x < 128 && row0 + line < rows) q.scale[(int64_t)(row0 + line) * q.ld_scale + tc] = scales[0][line];
+  if (QT && qt.block_rows == 1 && threadIdx.x >= 128 && col0 + line < cols) qt.scale[(int64_t)(col0 + line) * qt.ld_scale + tr] = scales[1][line];
+  if (QT) {
 #pragma unroll
     for (int p = 0; p < 4; p++) {
       const int cc = p * 32 + (threadIdx.x >> 3), k = threadIdx.x & 7, sw = cc >> 3;   // sw: the cx that wrote it

@@ -16,20 +16,21 @@ namespace {
 constexpr int NORM_MAX_D = 16384;
 constexpr int NORM_LAUNCH_ROWS = 1 << 21;   // of a launch of the forward pass: a grid has fewer than 2^32 threads
 
-__device__ __forceinline__ float norm_wave_sum(float v) {
+template <typename F>
+__device__ __forceinline__ F norm_wave_sum(F v) {
 #pragma unroll
   for (int o = 32; o > 0; o >>= 1) v += __shfl_xor(v, o, 64);
   return v;
 }
-// the sum over the NT threads that hold a row; sh: NT / 64 floats of their own
-template <int NT>
-__device__ __forceinline__ float row_sum(float v, float* sh) {
+// the sum over the NT threads that hold a row; sh: NT / 64 numbers of their own
+template <int NT, typename F>
+__device__ __forceinline__ F row_sum(F v, F* sh) {
   v = norm_wave_sum(v);
   if (NT == 64) return v;
   __syncthreads();   // the last reading of sh is over
   if ((threadIdx.x & 63) == 0) sh[threadIdx.x >> 6] = v;
   __syncthreads();
-  float s = sh[0];
+  F s = sh[0];
 #pragma unroll
   for (int i = 1; i < NT / 64; i++) s += sh[i];
   return s;
@@ -90,7 +91,7 @@ struct NormFwdArgs {
 // NT threads a row; NT = 64: four rows a workgroup
 template <typename T, int NT, int RUNS, bool CENTER>
 __global__ __launch_bounds__(NT == 64 ? 256 : NT) void norm_fwd_kernel(NormFwdArgs a) {
-  __shared__ float sh[NT / 64];
+  __shared__ double sh[NT / 64];
   const int t = NT == 64 ? threadIdx.x & 63 : threadIdx.x;
   const int row = NT == 64 ? blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6) : blockIdx.x;
   if (row >= a.rows) return;   // a whole wavefront, or nobody where the threads of a row meet
@@ -102,7 +103,6 @@ __global__ __launch_bounds__(NT == 64 ? 256 : NT) void norm_fwd_kernel(NormFwdAr
   gain.load(a.gain, a.d, t);
   x.settle(a.d, t);
   float v[RUNS][4];
-  float sum = 0.0f;
 #pragma unroll
   for (int s = 0; s < RUNS; s++)
 #pragma unroll
@@ -116,29 +116,30 @@ __global__ __launch_bounds__(NT == 64 ? 256 : NT) void norm_fwd_kernel(NormFwdAr
       store4(element(a.total + base, 4 * (t + NT * s)), a.d - 4 * (t + NT * s), v[s]);
     }
   }
-  if (CENTER)
+  // Sums of a row in double: what they are off by is the same for the whole row, and turns as many of its 8-bit values as lie that near to a border between two.
+  if (CENTER) {
+    double sum = 0.0;
 #pragma unroll
     for (int s = 0; s < RUNS; s++)
 #pragma unroll
-      for (int i = 0; i < 4; i++) sum += v[s][i];
-  if (CENTER) {
-    const float mean = row_sum<NT>(sum, sh) / (float)a.d;
+      for (int i = 0; i < 4; i++) sum += (double)v[s][i];
+    const double mean = row_sum<NT>(sum, sh) / a.d;
 #pragma unroll
     for (int s = 0; s < RUNS; s++)
 #pragma unroll
       for (int i = 0; i < 4; i++)
-        if (4 * (t + NT * s) + i < a.d) v[s][i] -= mean;
+        if (4 * (t + NT * s) + i < a.d) v[s][i] = (float)((double)v[s][i] - mean);
   }
-  float ss = 0.0f;
+  double ss = 0.0;
 #pragma unroll
   for (int s = 0; s < RUNS; s++)
 #pragma unroll
-    for (int i = 0; i < 4; i++) ss += v[s][i] * v[s][i];
+    for (int i = 0; i < 4; i++) ss = fma((double)v[s][i], (double)v[s][i], ss);
   ss = row_sum<NT>(ss, sh);
   // rstd in two parts, and each product with what its rounding left: an output in 8 bits turns an error of one rounding into a step of 1/16 where it falls on a border,
   // and what follows is rounded once.  (0.5 us of 40.)
   gain.settle(a.d, t);
-  const double rd = 1.0 / sqrt((double)ss / a.d + (double)a.eps);
+  const double rd = 1.0 / sqrt(ss / a.d + (double)a.eps);
   const float r = (float)rd, r_rest = (float)(rd - (double)r);
   if (t == 0) a.rstd[row] = r;
 #pragma unroll
