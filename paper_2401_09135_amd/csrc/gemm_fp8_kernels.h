@@ -110,9 +110,11 @@ __device__ __forceinline__ void zero_behind(char* row, int swizzle, int left) {
 constexpr int F8_STAGING = 32 * 128;
 __device__ __forceinline__ void fp8_order() { asm volatile("" ::: "memory"); }
 
-// How the kernel's results are written: bit 0: R is added, bit 1: C or R is not aligned for 16 bytes a lane.  Kernels of their own, as one that could do all keeps too few registers
-// for the products; tiles of 128 and 64 ask at run time (EPI_ASK).
-constexpr int EPI_ADD = 1, EPI_ANY = 2, EPI_ASK = 4;
+// How the kernel's results are written: bit 0: R is added, bit 1: C or R is not aligned for 16 bytes a lane, bit 3: where R is added, parts of 128 x 64 may end outside of the matrix.  Kernels of
+// their own, as one that could do all keeps too few registers for the products; tiles of 128 and 64 ask at run time (EPI_ASK).
+// In us, a kernel for all with R / these: 16384 x 896 x 3584 fp32 105 / 101, 16384 x 3584 x 896 fp32 178 / 168, 14638 x 6376 x 563 fp32 402 / 361 (8 rows of R at once at the edges), bf16
+// 16384 x 896 x 3584 without these kinds 90 / 66.
+constexpr int EPI_ADD = 1, EPI_ANY = 2, EPI_ASK = 4, EPI_EDGE = 8;
 template <int HOW, int TM, int TN, typename TO>
 __device__ __forceinline__ void fp8_epilogue(const f32x16 (&acc)[TM][TN], char* stg, const Fp8Args& g, TO* C, const float* R, int row0, int col0, int lane) {
   asm volatile("" : "+v"(lane));   // nothing of this is kept in registers from tile to tile
@@ -121,7 +123,7 @@ __device__ __forceinline__ void fp8_epilogue(const f32x16 (&acc)[TM][TN], char* 
   C += (int64_t)row0 * g.ldc + col0;
   if (add_r) R += (int64_t)row0 * g.ldr + col0;
   const int rows = g.M - row0, cols = g.N - col0;   // that are left
-  const bool full = rows >= TM * 32 && cols >= TN * 32;
+  const bool full = (HOW & (EPI_ADD | EPI_EDGE)) == EPI_ADD || (rows >= TM * 32 && cols >= TN * 32);
   const bool vec = full && (HOW & EPI_ASK ? fp8_aligned(g) : !(HOW & EPI_ANY));
   if (sizeof(TO) == 2 && TN == 2 && !add_r) {
     const unsigned off = (unsigned)((r8 * ldc + c8 * 8) * (int)sizeof(TO));
@@ -214,14 +216,21 @@ __device__ __forceinline__ void fp8_epilogue(const f32x16 (&acc)[TM][TN], char* 
           *reinterpret_cast<TO*>(reinterpret_cast<char*>(o) + off) = (TO)v;
         }
       } else {
-        const int n = rows - i * 32 < 32 ? rows - i * 32 : 32;
-        const float* x = add_r ? R + (int64_t)(i * 32) * g.ldr + j * 32 : nullptr;
-#pragma unroll 4
-        for (int r = hf; r < n; r += 2) {
-          float v = *reinterpret_cast<const float*>(stg + r * 128 + ((wr >> 2) ^ (r & 7)) * 16 + (wr & 3) * 4);
-          if (j * 32 + wr < cols) {
-            if (add_r) v += x[(int64_t)r * g.ldr + wr];
-            o[(int64_t)r * g.ldc + wr] = (TO)v;
+        const int n = rows - i * 32 < 32 ? rows - i * 32 : 32, m = cols - j * 32;   // rows and columns of the block
+        if (m > 0) {
+          constexpr int U = 8;   // rows of a half of the wavefront under way at once; those behind the last are the last, so that their loads need no branch
+          const float* from = add_r ? R + (int64_t)(i * 32) * g.ldr + j * 32 + (wr < m ? wr : m - 1) : nullptr;
+#pragma unroll 1
+          for (int r0 = hf; r0 < n + hf; r0 += 2 * U) {
+            float x[U];
+#pragma unroll
+            for (int u = 0; u < U; u++) x[u] = add_r ? from[(int64_t)(r0 + 2 * u < n ? r0 + 2 * u : n - 1) * g.ldr] : 0.0f;
+#pragma unroll
+            for (int u = 0; u < U; u++) {
+              const int r = r0 + 2 * u;
+              const float v = *reinterpret_cast<const float*>(stg + (r & 31) * 128 + ((wr >> 2) ^ (r & 7)) * 16 + (wr & 3) * 4);
+              if (r < n && wr < m) o[(int64_t)r * g.ldc + wr] = (TO)(add_r ? v + x[u] : v);
+            }
           }
         }
       }
@@ -689,11 +698,13 @@ inline int launch_fp8(Fp8Args g, int tile, hipStream_t st) {
     if constexpr (!WIDE && sizeof(TO) == 4) {     // partial sums, aligned
       hipLaunchKernelGGL((gemm_fp8_pp_kernel<FA, FB, WIDE, TO, 0>), grid, dim3(512), 0, st, g, tiles);
     } else {
-      const int how = (g.r ? EPI_ADD : 0) | (fp8_aligned(g) ? 0 : EPI_ANY);
+      const bool whole = g.M % 128 == 0 && g.N % 64 == 0;   // no wavefront's part of a tile ends outside
+      const int how = (g.r ? EPI_ADD : 0) | (fp8_aligned(g) ? 0 : EPI_ANY) | (g.r && !(whole && fp8_aligned(g)) ? EPI_EDGE : 0);
       if (how == 0) hipLaunchKernelGGL((gemm_fp8_pp_kernel<FA, FB, WIDE, TO, 0>), grid, dim3(512), 0, st, g, tiles);
       else if (how == EPI_ADD) hipLaunchKernelGGL((gemm_fp8_pp_kernel<FA, FB, WIDE, TO, EPI_ADD>), grid, dim3(512), 0, st, g, tiles);
+      else if (how == (EPI_ADD | EPI_EDGE)) hipLaunchKernelGGL((gemm_fp8_pp_kernel<FA, FB, WIDE, TO, EPI_ADD | EPI_EDGE>), grid, dim3(512), 0, st, g, tiles);
       else if (how == EPI_ANY) hipLaunchKernelGGL((gemm_fp8_pp_kernel<FA, FB, WIDE, TO, EPI_ANY>), grid, dim3(512), 0, st, g, tiles);
-      else hipLaunchKernelGGL((gemm_fp8_pp_kernel<FA, FB, WIDE, TO, EPI_ADD | EPI_ANY>), grid, dim3(512), 0, st, g, tiles);
+      else hipLaunchKernelGGL((gemm_fp8_pp_kernel<FA, FB, WIDE, TO, EPI_ADD | EPI_ANY | EPI_EDGE>), grid, dim3(512), 0, st, g, tiles);
     }
   } else if (tile == 128) hipLaunchKernelGGL((gemm_fp8_deep_kernel<FA, FB, WIDE, TO, 128, 128, 4>), dim3(tiles), dim3(Fp8Deep<128, 128, 4>::NT), 0, st, g);
   else hipLaunchKernelGGL((gemm_fp8_deep_kernel<FA, FB, WIDE, TO, 64, 64, 4>), dim3(tiles), dim3(Fp8Deep<64, 64, 4>::NT), 0, st, g);

@@ -301,7 +301,7 @@ def test_product_of_whole_numbers_is_exact(M, N, K, fa, fb, ra, rb, with_ws):
     assert torch.equal(rc.cpu().double(), want + r.double())
 
 
-VARIANT_SIZES = [(1, 1, 1), (65, 63, 130), (100, 257, 15), (257, 511, 385), (513, 100, 2049), (300, 1000, 48), (31, 2000, 4097), (1500, 40, 3000), (640, 896, 640), (1100, 2100, 1500)]
+VARIANT_SIZES = [(1, 1, 1), (65, 63, 130), (100, 257, 15), (257, 511, 385), (513, 100, 2049), (300, 1000, 48), (31, 2000, 4097), (1500, 40, 3000), (640, 896, 640), (1100, 2100, 1500), (128, 64, 128), (384, 320, 256), (896, 448, 100), (129, 64, 300), (256, 65, 300)]
 
 
 @pytest.mark.parametrize("tile", [256, 128, 64])
