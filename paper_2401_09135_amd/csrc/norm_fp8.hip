@@ -181,6 +181,7 @@ template <typename T, int NT, int RUNS, bool CENTER>
 __global__ __launch_bounds__(NT == 64 ? 256 : NT) void norm_bwd_kernel(NormBwdArgs a) {
   constexpr int AT_ONCE = NT == 64 ? 4 : 1;
   __shared__ float sh[NT / 64];
+  __shared__ double sh_mean[CENTER ? NT / 64 : 1];
   __shared__ float parts[NT == 64 ? 3 : 1][NT == 64 ? 1024 : 1];
   const int t = NT == 64 ? threadIdx.x & 63 : threadIdx.x, w = NT == 64 ? __builtin_amdgcn_readfirstlane(threadIdx.x >> 6) : 0;
   const float inv_d = 1.0f / (float)a.d;
@@ -223,25 +224,30 @@ __global__ __launch_bounds__(NT == 64 ? 256 : NT) void norm_bwd_kernel(NormBwdAr
     dy.settle(d, t);
     const float r = rstd;
     float x[RUNS][4], h[RUNS][4];
-    float sx = 0.0f, sh1 = 0.0f, dot = 0.0f;
+    double sx = 0.0;
+    float sh1 = 0.0f, dot = 0.0f;
 #pragma unroll
     for (int s = 0; s < RUNS; s++)
 #pragma unroll
       for (int i = 0; i < 4; i++) {
         x[s][i] = total.at(s, i, d, t);
         h[s][i] = dy.at(s, i, d, t);
-        if (CENTER) sx += x[s][i];
+        if (CENTER) sx += (double)x[s][i];
       }
     RowPart<float, NT, RUNS> add = in;
     if (AHEAD) load(row + stride);
-    const float mean = CENTER ? row_sum<NT>(sx, sh) * inv_d : 0.0f;
+    // The mean in double, as in the forward pass: what it is off by is the same for the whole row, adds up in the gain's gradient, and is in fp32 a rounding times the mean over
+    // the spread (rows of 896 with a mean of 1000 spreads: xh off by 5e-5 in the mean, 1.5e-4 at most).  16384 x 896 takes 40.5 us so and 39.8 in fp32, 2000 x 8192 56.7 and 54, 1000 x
+    // 16000 64 and 61 (LayerNorm, bf16 dy).  The mean is taken off in two parts, halved with the row where the difference could leave fp32's range.
+    const double mean = CENTER ? row_sum<NT>(sx, sh_mean) / d : 0.0;
+    const float whole = (float)mean, half = fabsf(whole) > 0x1p100f ? 0.5f : 1.0f, off = -whole * half, rest = (float)(mean - (double)whole) * half, rc = half < 1.0f ? r * 2.0f : r;
 #pragma unroll
     for (int s = 0; s < RUNS; s++) {
       if (!AHEAD) gain.v[s] = kept[0][s][t];
       f32x4 sum = AHEAD ? (f32x4){dg[s][0], dg[s][1], dg[s][2], dg[s][3]} : kept[1][s][t];
 #pragma unroll
       for (int i = 0; i < 4; i++) {
-        x[s][i] = (CENTER ? x[s][i] - mean : x[s][i]) * r;   // xh; outside the row h is 0
+        x[s][i] = (CENTER ? fmaf(x[s][i], half, off) - rest : x[s][i]) * rc;   // xh; outside the row h is 0
         sum[i] += h[s][i] * x[s][i];
         h[s][i] *= gain.at(s, i, d, t);
         sh1 += h[s][i];
