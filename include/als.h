@@ -314,7 +314,8 @@ int als_k_quant_fp8(const void* x, int dtype, int rows, int cols, int64_t ldx, c
 /* Norm of x + resid in one pass, for up to 2^30 rows of d <= 16384 elements: total = x + resid; y = total rstd gain (ALS_NORM_RMS; ALS_NORM_LAYER: total
  * minus its mean), rstd = 1 / sqrt(mean of squares + eps).  x in dtype, resid and total fp32, all [rows, d] without padding; resid and total are both null
  * (then total is x) or neither; total may be resid, or x in fp32.  y (bf16 [rows, d]) and q (8 bits with block_rows 1, formed from y before its rounding) may
- * be null, not both.  rstd [rows] is what the backward pass takes. */
+ * be null, not both.  rstd [rows] is what the backward pass takes.  All between total and an output's rounding is in double: no total that fp32 holds is too large or too small
+ * (rstd, in fp32, is infinite for rows under 3e-39 without an eps; their y and q are right, a backward pass with such an rstd has no meaning). */
 int als_k_norm_fwd(const void* x, int dtype, const float* resid, const float* gain, float* total, void* y, const als_fp8* q, float* rstd,
                    int rows, int d, double eps, int norm_kind, void* stream);
 /* Its backward pass, with y's gradient dy (dtype) as if y were not rounded: ds = ds_in + rstd (h - xh mean(h xh)), h = dy gain, xh = total rstd
