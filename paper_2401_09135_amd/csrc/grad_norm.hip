@@ -117,8 +117,8 @@ __global__ __launch_bounds__(256) void grad_squares_kernel(GradTable t, double* 
   if (threadIdx.x == 0) partial[blockIdx.x] = sh[0] + sh[1] + sh[2] + sh[3];
 }
 
-__global__ __launch_bounds__(1024) void grad_norm_kernel(const double* __restrict__ partial, int64_t n, float* __restrict__ norm, float* log, const StepState* ss,
-                                                         int64_t log_offset) {
+// also leaves the norm in double in partial[0], if there is one
+__global__ __launch_bounds__(1024) void grad_norm_kernel(double* partial, int64_t n, float* __restrict__ norm, float* log, const StepState* ss, int64_t log_offset) {
   __shared__ double sh[16];
   double s = 0.0;
   for (int64_t i = threadIdx.x; i < n; i += 1024) s += partial[i];
@@ -127,56 +127,60 @@ __global__ __launch_bounds__(1024) void grad_norm_kernel(const double* __restric
   __syncthreads();
   if (threadIdx.x == 0) {
     for (int i = 1; i < 16; i++) s += sh[i];
-    const float root = (float)sqrt(s);
-    norm[0] = root;
+    s = sqrt(s);
+    norm[0] = (float)s;
+    if (n) partial[0] = s;   // every sum has been read
     if (ss) log = ss->loss_out + ss->step + log_offset;
-    if (log) log[0] = root;
+    if (log) log[0] = (float)s;
   }
 }
 
 template <typename T>
-__device__ __forceinline__ void scale_pieces(const void* in, void* out, int64_t numel, int64_t p0, int64_t p1, float k) {
+__device__ __forceinline__ void scale_pieces(const void* in, void* out, int64_t numel, int64_t p0, int64_t p1, double k) {
   constexpr int E = Pieces<T>::E;
   const Pieces<T> x(in, numel);
   if (p1 > x.count) p1 = x.count;
   T* o = (T*)out - x.lead;   // element i of piece p goes to o[p E + i]
   const bool aligned = ((uintptr_t)o % 16) == 0;
+  auto scaled = [k](float g) { return (float)((double)g * k); };
   for (int64_t p = p0 + threadIdx.x; p < p1; p += 256) {
     float v[E];
     x.load(p, v);
     if (aligned && x.whole(p)) {
       if constexpr (sizeof(T) == 4) {
-        reinterpret_cast<f32x4*>(o)[p] = (f32x4){v[0] * k, v[1] * k, v[2] * k, v[3] * k};
+        reinterpret_cast<f32x4*>(o)[p] = (f32x4){scaled(v[0]), scaled(v[1]), scaled(v[2]), scaled(v[3])};
       } else {
         bf16x8 y;
 #pragma unroll
-        for (int e = 0; e < E; e++) y[e] = (bf16)(v[e] * k);
+        for (int e = 0; e < E; e++) y[e] = (bf16)scaled(v[e]);
         reinterpret_cast<bf16x8*>(o)[p] = y;
       }
     } else {
 #pragma unroll
       for (int e = 0; e < E; e++)
-        if (x.has(p, e)) o[p * E + e] = (T)(v[e] * k);
+        if (x.has(p, e)) o[p * E + e] = (T)scaled(v[e]);
     }
   }
 }
 
-// count: partial sums that each workgroup adds itself, in the order of grad_norm_kernel, the first one leaving the norm; 0: the norm is there
-__global__ __launch_bounds__(256) void grad_clip_kernel(GradTable t, float* norm, float max_norm, const double* __restrict__ partial, int count) {
-  float root;
+// count: partial sums that each workgroup adds itself, in the order of grad_norm_kernel, the first one leaving the norm; 0: the norm is in partial[0].  The coefficient and the
+// products with it are in double: a norm of finite gradients can leave fp32's range, and an output is then what it is there, and rounded once (10^8 elements of
+// fp32 255 us, 253.6 in fp32).
+__global__ __launch_bounds__(256) void grad_clip_kernel(GradTable t, float* norm, double max_norm, const double* __restrict__ partial, int count) {
+  double root;
   if (count) {
     __shared__ double sh[4];
     const double s = wave_sum_f64((int)threadIdx.x < count ? partial[threadIdx.x] : 0.0);
     if ((threadIdx.x & 63) == 0) sh[threadIdx.x >> 6] = s;
     __syncthreads();
-    root = (float)sqrt(sh[0] + sh[1] + sh[2] + sh[3]);
-    if (blockIdx.x == 0 && threadIdx.x == 0) norm[0] = root;
+    root = sqrt(sh[0] + sh[1] + sh[2] + sh[3]);
+    if (blockIdx.x == 0 && threadIdx.x == 0) norm[0] = (float)root;
   } else {
-    root = norm[0];
+    root = partial[0];
   }
-  const float k = clip_coefficient(root, max_norm);
+  const double k = root <= max_norm ? 1.0 : max_norm / root;
   for_chunks(t, [&](const void* in, void* out, int64_t numel, bool bf, int64_t p0, int64_t p1) {
-    if (k == 1.0f && in == out) return;   // nothing changes
+    if (k == 1.0 && in == out) return;   // nothing changes
     if (bf) scale_pieces<bf16>(in, out, numel, p0, p1, k);
     else scale_pieces<float>(in, out, numel, p0, p1, k);
   });
@@ -324,7 +328,7 @@ extern "C" int als_k_grad_clip(int n, const void* const* grads, void* const* out
     ALS_CHECK_LAUNCH();
   }
   return for_launches(n, grads, outs, numel, dtypes, [&](const GradTable& t, int blocks, int64_t) {
-    hipLaunchKernelGGL(grad_clip_kernel, dim3(blocks), dim3(256), 0, st, t, norm_out, (float)max_norm, partial, again);
+    hipLaunchKernelGGL(grad_clip_kernel, dim3(blocks), dim3(256), 0, st, t, norm_out, max_norm, partial, again);
     ALS_CHECK_LAUNCH();
     return ALS_OK;
   });
