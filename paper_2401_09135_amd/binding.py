@@ -1,5 +1,6 @@
 """ctypes binding with the same names as the C ABI in include/als.h (argument marshalling
-only).  torch supplies device buffers and streams."""
+only).  torch supplies device buffers and streams: a k_* call runs on `stream`, and without one on
+torch's current stream; a tensor that another stream uses is the caller's to wait for and to keep."""
 from __future__ import annotations
 
 import array
@@ -195,8 +196,14 @@ def shard_sample(sizes, learned, u: float):
     return p[:s.size], int(pick[0])
 
 
+_raw_stream, _gpu = torch._C._cuda_getCurrentRawStream, torch._C._cuda_getDevice   # without torch.cuda's own checks: 0.2 us of a call's 5
+
+
 def _stream_handle(stream) -> int:
-    return 0 if stream is None else int(stream.cuda_stream)
+    """A torch stream's handle; None: that of torch's current stream (on the current GPU), as torch's own calls take it."""
+    if stream is None:
+        return _raw_stream(_gpu())
+    return int(stream.cuda_stream)
 
 
 class Context:
@@ -225,7 +232,7 @@ class Context:
         else:
             n_streams = cfg.n_workers if n_streams is None else n_streams
             self.streams = [torch.cuda.Stream(device=self.device) for _ in range(n_streams)]
-        handles = (_P * n_streams)(*[_stream_handle(s) for s in self.streams])
+        handles = (_P * n_streams)(*[s.cuda_stream if s is not None else 0 for s in self.streams])
         torch.cuda.synchronize()
         self._ctx = _P()
         _check(lib.als_init(C.byref(cfg), base, nbytes, _np_ptr(theta0), handles, n_streams, C.byref(self._ctx)))
@@ -591,15 +598,21 @@ def _either(what, t, numel=None):
 _gpus = 0
 
 
-def _call(dev, fn, *args):
-    """The call with that GPU as the current one."""
+def _call(what, dev, stream, fn, *args):
+    """The call with that GPU as the current one, on the stream (None: torch's current one on that GPU)."""
     global _gpus
-    _gpus = _gpus or torch.cuda.device_count()
-    if _gpus > 1 and dev >= 0 and dev != torch.cuda.current_device():
-        with torch.cuda.device(dev):
-            rc = fn(*args)
+    if stream is None:
+        handle = _raw_stream(dev)
     else:
-        rc = fn(*args)
+        handle = int(stream.cuda_stream)
+        if getattr(stream, "device_index", dev) != dev:
+            raise AlsError(f"{what}: the stream must be of the GPU that the tensors are on")
+    _gpus = _gpus or torch.cuda.device_count()
+    if _gpus > 1 and dev != _gpu():
+        with torch.cuda.device(dev):
+            rc = fn(*args, handle)
+    else:
+        rc = fn(*args, handle)
     if rc:
         _check(rc)
 
@@ -624,8 +637,8 @@ def k_quant_fp8(x, q=None, qt=None, stream=None):
         raise AlsError("k_quant_fp8: x must be a matrix of fp32 or bf16 with unit column stride")
     if (q is not None and q.shape != (rows, cols)) or (qt is not None and qt.shape != (cols, rows)):
         raise AlsError("k_quant_fp8: q must be [rows, cols] and qt [cols, rows]")
-    _call(_device("k_quant_fp8", x, q, qt), lib.als_k_quant_fp8, x.data_ptr(), code, rows, cols, ldx, q._ref if q is not None else None,
-          qt._ref if qt is not None else None, _stream_handle(stream))
+    _call("k_quant_fp8", _device("k_quant_fp8", x, q, qt), stream, lib.als_k_quant_fp8, x.data_ptr(), code, rows, cols, ldx, q._ref if q is not None else None,
+          qt._ref if qt is not None else None)
 
 
 NORM_KINDS = {"rms": 0, "layer": 1}
@@ -646,8 +659,8 @@ def k_norm_fwd(x, gain, resid=None, total=None, y=None, q=None, rstd=None, norm=
         raise AlsError("k_norm_fwd: q must be [rows, d]")
     dev = _device(what, x, gain, resid, total, y, q, rstd)
     px, code = _either(what, x)
-    _call(dev, lib.als_k_norm_fwd, px, code, _flat(what, resid, f32, n), _flat(what, gain, f32, d), _flat(what, total, f32, n),
-          _flat(what, y, torch.bfloat16, n), q._ref if q is not None else None, _flat(what, rstd, f32, rows), rows, d, eps, NORM_KINDS[norm], _stream_handle(stream))
+    _call(what, dev, stream, lib.als_k_norm_fwd, px, code, _flat(what, resid, f32, n), _flat(what, gain, f32, d), _flat(what, total, f32, n),
+          _flat(what, y, torch.bfloat16, n), q._ref if q is not None else None, _flat(what, rstd, f32, rows), rows, d, eps, NORM_KINDS[norm])
 
 
 def k_norm_bwd_ws_bytes(rows: int, d: int) -> int:
@@ -661,8 +674,8 @@ def k_norm_bwd(dy, total, rstd, gain, ds, dgain, ws, ds_in=None, ds_lp=None, nor
     n = rows * d
     dev = _device(what, dy, total, rstd, gain, ds, dgain, ws, ds_in, ds_lp)
     p, code = _either(what, dy)
-    _call(dev, lib.als_k_norm_bwd, p, code, _flat(what, total, f32, n), _flat(what, rstd, f32, rows), _flat(what, gain, f32, d), _flat(what, ds_in, f32, n),
-          _flat(what, ds, f32, n), _flat(what, ds_lp, torch.bfloat16, n), _flat(what, dgain, f32, d), rows, d, NORM_KINDS[norm], *_ws(what, ws), _stream_handle(stream))
+    _call(what, dev, stream, lib.als_k_norm_bwd, p, code, _flat(what, total, f32, n), _flat(what, rstd, f32, rows), _flat(what, gain, f32, d), _flat(what, ds_in, f32, n),
+          _flat(what, ds, f32, n), _flat(what, ds_lp, torch.bfloat16, n), _flat(what, dgain, f32, d), rows, d, NORM_KINDS[norm], *_ws(what, ws))
 
 
 def k_gemm_fp8_ws_bytes(M: int, N: int, K: int) -> int:
@@ -692,7 +705,7 @@ def k_gemm_fp8(a, b, c, resid=None, ws=None, stream=None):
             unit = unit_r
     if (N > 1 and unit != 1) or ldc < N or (pr and ldr < N):
         raise AlsError("k_gemm_fp8: c and resid must have unit column stride")
-    _call(_device(what, a, b, c, resid, ws), lib.als_k_gemm_fp8, a._ref, b._ref, c.data_ptr(), ldc, code, pr or None, ldr, M, N, K, *_ws(what, ws), _stream_handle(stream))
+    _call(what, _device(what, a, b, c, resid, ws), stream, lib.als_k_gemm_fp8, a._ref, b._ref, c.data_ptr(), ldc, code, pr or None, ldr, M, N, K, *_ws(what, ws))
 
 
 lib.als_k_set_gemm_fp8.argtypes = [C.c_int, C.c_int]
@@ -743,7 +756,7 @@ def k_grad_norm(grads, norm, ws, stream=None):
     dev = _device(what, norm, ws)
     p, numel, dtypes = _grad_list(what, grads, dev)
     (ap, p), (an, numel_p), at = _addresses(p), _addresses(numel), array.array("i", dtypes)
-    _call(dev, lib.als_k_grad_norm, len(grads), p, numel_p, at.buffer_info()[0], _flat(what, norm, torch.float32, 1), *_ws(what, ws), _stream_handle(stream))
+    _call(what, dev, stream, lib.als_k_grad_norm, len(grads), p, numel_p, at.buffer_info()[0], _flat(what, norm, torch.float32, 1), *_ws(what, ws))
 
 
 def k_grad_clip(grads, outs, max_norm, norm, ws, stream=None):
@@ -755,13 +768,12 @@ def k_grad_clip(grads, outs, max_norm, norm, ws, stream=None):
     if numel_o != numel or dtypes_o != dtypes:
         raise AlsError("k_grad_clip: outs must match grads in number, sizes and types")
     (ap, p), (ao, po), (an, numel_p), at = _addresses(p), _addresses(po), _addresses(numel), array.array("i", dtypes)
-    _call(dev, lib.als_k_grad_clip, len(grads), p, po, numel_p, at.buffer_info()[0], float(max_norm), _flat(what, norm, torch.float32, 1), *_ws(what, ws),
-          _stream_handle(stream))
+    _call(what, dev, stream, lib.als_k_grad_clip, len(grads), p, po, numel_p, at.buffer_info()[0], float(max_norm), _flat(what, norm, torch.float32, 1), *_ws(what, ws))
 
 
 def k_adamw_clip(theta, grad, m, v, bf16_out, P_decay, step, lr, norm, max_norm, beta1=0.9, beta2=0.999, eps=1e-8, wd=0.1, stream=None):
     """k_adamw with the gradient scaled so that its norm (norm[0], on the GPU: k_grad_norm) is at most max_norm."""
     what, f32, P = "k_adamw_clip", torch.float32, theta.numel()
     dev = _device(what, theta, grad, m, v, bf16_out, norm)
-    _call(dev, lib.als_k_adamw_clip, _flat(what, theta, f32, P), _flat(what, grad, f32, P), _flat(what, m, f32, P), _flat(what, v, f32, P),
-          _flat(what, bf16_out, torch.bfloat16, P), P, P_decay, step, lr, beta1, beta2, eps, wd, _flat(what, norm, f32, 1), max_norm, _stream_handle(stream))
+    _call(what, dev, stream, lib.als_k_adamw_clip, _flat(what, theta, f32, P), _flat(what, grad, f32, P), _flat(what, m, f32, P), _flat(what, v, f32, P),
+          _flat(what, bf16_out, torch.bfloat16, P), P, P_decay, step, lr, beta1, beta2, eps, wd, _flat(what, norm, f32, 1), max_norm)
