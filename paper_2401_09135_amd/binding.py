@@ -505,9 +505,13 @@ lib.als_k_adamw_clip.argtypes = [_P, _P, _P, _P, _P, C.c_int64, C.c_int64, C.c_i
 class Fp8:
     """A matrix in 8-bit floating point on the device (als_fp8): data [rows, cols] float8_e4m3fn or float8_e5m2 with unit
     column stride, rows a multiple of 16 bytes apart; scale [ceil(rows / block_rows), ceil(cols / 128)] float8_e8m0fnu,
-    rows a multiple of 4 bytes apart; block_rows 1 or 128.  Views of wider buffers are taken: see empty()."""
+    rows a multiple of 4 bytes apart; block_rows 1 or 128.  Views of wider buffers are taken: see empty().  It stands for the memory
+    that these tensors had when it was made: others cannot be put in their place, and once one has been given other memory calls refuse it."""
 
-    __slots__ = ("data", "scale", "block_rows", "shape", "device_index", "_c", "_ref")
+    __slots__ = ("_data", "_scale", "_block_rows", "shape", "device_index", "_c", "_ref")
+    data = property(lambda self: self._data)
+    scale = property(lambda self: self._scale)
+    block_rows = property(lambda self: self._block_rows)
 
     def __init__(self, data, scale, block_rows: int = 1):
         fmt = _FP8_DTYPES.get(data.dtype)
@@ -523,7 +527,7 @@ class Fp8:
         if scale.shape != (s_rows, s_cols):
             raise AlsError("Fp8: scale must be [ceil(rows / block_rows), ceil(cols / 128)] of data [rows, cols]")
         self.device_index = _device("Fp8", data, scale)
-        self.data, self.scale, self.block_rows = data, scale, block_rows
+        self._data, self._scale, self._block_rows = data, scale, block_rows
         p, ld = _rows_of("Fp8: data", data, rows, cols, 16)
         ps, ld_scale = _rows_of("Fp8: scale", scale, s_rows, s_cols, 4)
         self._c = s = _Fp8Struct(p, ps, ld, ld_scale, fmt, block_rows)
@@ -532,7 +536,9 @@ class Fp8:
     @classmethod
     def empty(cls, rows: int, cols: int, format: str = "e4m3", block_rows: int = 1, device="cuda:0") -> "Fp8":
         up = lambda n, m: -(-n // m) * m
-        dt = {"e4m3": torch.float8_e4m3fn, "e5m2": torch.float8_e5m2}[format]
+        dt = {"e4m3": torch.float8_e4m3fn, "e5m2": torch.float8_e5m2}.get(format)
+        if dt is None or (block_rows != 1 and block_rows != 128) or rows < 0 or cols < 0:
+            raise AlsError(f"Fp8: format must be 'e4m3' or 'e5m2', block_rows 1 or 128, rows and cols at least 0, got {format!r}, {block_rows}, {rows}, {cols}")
         kb = -(-cols // 128)
         data = torch.empty(rows, up(cols, 16), dtype=torch.uint8, device=device).view(dt)[:, :cols]
         scale = torch.empty(-(-rows // block_rows), up(kb, 4), dtype=torch.uint8, device=device).view(torch.float8_e8m0fnu)[:, :kb]
@@ -563,7 +569,12 @@ def _device(what, *tensors):
     dev = -1
     for t in tensors:
         if t is not None:
-            d = t.device_index if type(t) is Fp8 else t.get_device()
+            if type(t) is Fp8:
+                d, c = t.device_index, t._c
+                if t._data.data_ptr() != (c.data or 0) or t._scale.data_ptr() != (c.scale or 0):
+                    raise AlsError(f"{what}: the data or scale of an Fp8 have other memory than when it was made")
+            else:
+                d = t.get_device()
             if d < 0:
                 raise AlsError(f"{what}: tensors must be on the GPU")
             if d != dev:
