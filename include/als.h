@@ -205,7 +205,8 @@ int als_sync(als_ctx* ctx, int worker);
 /* Losses of the worker's most recent als_worker_local_steps call (n <= its n_steps). */
 int als_get_losses(als_ctx* ctx, int worker, float* host_out, int n);
 /* Gradient clipping of the local steps that are enqueued from now on: a step's gradient, over all parameters, is multiplied by max_norm / norm if its
- * norm exceeds max_norm (> 0), before AdamW (a norm beyond fp32's range is infinite: the gradient is then multiplied by 0).  0, as after als_init: off.  ALS_VEC_GRAD keeps the gradient as it was before.  A worker whose
+ * norm exceeds max_norm (> 0), before AdamW (a norm beyond fp32's range is infinite: the gradient is then multiplied by 0).  0, as after als_init: off.  With
+ * clipping on, AdamW is that of als_k_adamw_clip, also in steps that it leaves as they are: their results differ in the last digits from those with it off.  ALS_VEC_GRAD keeps the gradient as it was before.  A worker whose
  * steps are replayed has its graph captured anew: the call then waits for all workers, and is refused
  * while a measurement hook is in force. */
 int als_set_grad_clip(als_ctx* ctx, double max_norm);
@@ -350,7 +351,9 @@ int als_k_grad_norm(int n, const void* const* grads, const int64_t* numel, const
  * grad_i, and must not overlap any other tensor: refused. */
 int als_k_grad_clip(int n, const void* const* grads, void* const* outs, const int64_t* numel, const int32_t* dtypes, double max_norm,
                     float* norm_out, void* ws_dev, size_t ws_bytes, void* stream);
-/* als_k_adamw with the gradient times that coefficient, from a norm on the device: clipping without a pass of its own.  The norm is taken as it stands there, in fp32, and
+/* AdamW's step (als_k_adamw) with the gradient times that coefficient, from a norm on the device: clipping without a pass of its own.  1 - beta is rounded from double here, while
+ * als_k_adamw forms it in fp32 (1 - 0.999f is 1.3e-5 below 0.001, 1 - 0.9f 2.4e-7 above 0.1): where nothing is clipped, the gradient's share of v is that much larger here, of m
+ * that much smaller, and results are not als_k_adamw's to the last bit.  The norm is taken as it stands there, in fp32, and
  * the coefficient formed in fp32: one beyond its range is infinite and gives 0. */
 int als_k_adamw_clip(float* theta, const float* grad, float* m, float* v, void* bf16_out, int64_t P, int64_t P_decay, int64_t step,
                      double lr, double beta1, double beta2, double eps, double wd, const float* norm_dev, double max_norm, void* stream);

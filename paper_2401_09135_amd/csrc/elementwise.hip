@@ -116,7 +116,8 @@ __global__ void adamw_tail_kernel(float* theta, const float* grad, float* m, flo
   if (lp) lp[i] = (bf16)th;
 }
 
-// adam_one with 1 - beta rounded from double: 1 - 0.999f, formed in fp32, is 1.3e-5 below 0.001, and so would v and v's own gradient's share be.
+// adam_one with 1 - beta rounded from double: 1 - 0.999f, formed in fp32, is 1.3e-5 below 0.001, and so would the gradient's share of v be.  (adam_one forms it so, as
+// the oracle in fp32 does, whose steps it has to give.)
 __device__ __forceinline__ void adam_one_clipped(float& th, float g, float& m, float& v, bool decay, const AdamArgs& a, const ClipArgs& c) {
   m = a.beta1 * m + c.rest1 * g;
   v = a.beta2 * v + c.rest2 * g * g;

@@ -60,3 +60,24 @@ def test_clipped_gradients_are_rounded_once(sizes, dtypes):
     outs = [torch.full_like(t, 7.0) for t in grads]
     clip(grads, outs, want * (1 + 1e-12))
     assert all(torch.equal(a, b) for a, b in zip(outs, grads))
+
+
+@pytest.mark.parametrize("P", [4, 4099, 100000])
+def test_a_limit_that_does_not_bind_changes_adamw_by_its_constants_alone(P):
+    """1 - beta rounded from double behind a norm, and formed in fp32 without: of the gradient's share of v 1.3e-5, of m 2.4e-7."""
+    g = torch.Generator().manual_seed(P)
+    th, gr, m, v = torch.randn(P, generator=g), torch.randn(P, generator=g), 0.1 * torch.randn(P, generator=g), torch.rand(P, generator=g) * 1e-4
+    plain, clipped = ([t.to(DEV) for t in (th, gr, m, v)] for _ in range(2))
+    A.k_adamw(*plain, None, P // 2, 3, 1e-3)
+    A.k_adamw_clip(*clipped, None, P // 2, 3, 1e-3, torch.ones(1, device=DEV), 2.0)
+    f = lambda x: float(torch.tensor(x, dtype=F))  # noqa: E731
+    more = [f(1 - b) - float(torch.tensor(1.0) - torch.tensor(b, dtype=F)) for b in (0.9, 0.999)]
+    # 0.1 itself is rounded by 1.5e-9, 1.5e-8 of it, and the figure by 2e-9 of it
+    assert abs(more[0] / 0.1 + 2.4e-7) < 1.5e-8 + 2e-9 and abs(more[1] / 0.001 - 1.29e-5) < 1e-7
+    x = gr.double()
+    for i, old, share, by in ((2, m.double().abs(), x.abs(), more[0] * x), (3, v.double(), 0.001 * x * x, more[1] * x * x)):
+        # five roundings a side: two products of the gradient, one of what was there, the sum
+        assert (clipped[i].cpu().double() - plain[i].cpu().double() - by).abs().le(10 * U * (old + share)).all()
+    # m / sqrt(v) moves by at most the first and half of the second, and by some roundings
+    moved = 1e-3 * (clipped[2].cpu().double().abs() / 0.271) / torch.sqrt(clipped[3].cpu().double() / 0.002997)
+    assert (clipped[0].cpu().double() - plain[0].cpu().double()).abs().le(moved * (0.7e-5 + 30 * U) + 4 * U * (th.double().abs() + 1e-3)).all()
