@@ -329,8 +329,10 @@ int als_k_norm_bwd(const void* dy, int dtype, const float* total, const float* r
 
 /* C = A.B^T (+ R) of matrices in 8 bits: A [M, K], B [N, K] (the contraction runs along the rows of both, so a weight matrix stored
  * [K, N] is taken as its transposed form), any two formats and block_rows.  fp32 results: exact products of elements from 2^-126 to 2^127, summed in fp32.  bf16
- * results: the 8-bit matrix instruction, at up to twice the rate; it sums in fp32 too, but among 8 neighbours in K a product under 2^-13 of the largest may be
- * lost (1.5e-5 of a sum of random signs; a rounding to bf16 is up to 4e-3).  C [M, N] in out_dtype, rows ldc elements
+ * results: the 8-bit matrix instruction, at up to twice the rate; it sums in fp32 too, but among 8 neighbours in K each product is
+ * cut, towards zero, to 2^-13 of the largest.  That loses nothing where those 8 are within 2^6 of one another, less than 8.5e-4 of the sum of magnitudes
+ * whatever they are, and of K = 8192: 1.5e-5 of a sum of normal numbers of random sign, 7e-5 with outliers or magnitudes over five decades; sums of one sign are too small by 3e-6
+ * and 1e-4.  (A rounding to bf16 is up to 4e-3; one result in 60 is another bf16 neighbour than with exact sums.)  Where that matters take fp32 results.  C [M, N] in out_dtype, rows ldc elements
  * apart; R (fp32, rows ldr apart) may be null, and may be C itself if that is fp32 and ldr is ldc.  K = 0 gives R or zeros.  M, K <= 2^30, N <= 2^20, ld and ld_scale
  * <= 2^23, ldc and ldr <= 2^26.
  * ws_dev (256-byte aligned, may be null): scratch for the partial sums of products that are split along K; als_k_gemm_fp8_ws_bytes is what

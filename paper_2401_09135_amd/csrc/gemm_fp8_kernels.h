@@ -2,8 +2,9 @@
 //
 // bf16 results: v_mfma_scale_f32_32x32x64_f8f6f4 takes a scale byte for each row and 32 elements of K of either operand and adds to fp32, so the
 // scales cost no vector instruction.  It cuts each product to 2^-13 of the largest of the 8 neighbours in K that it adds first (measured: 2^16 + 4 is
-// 2^16 where the two are among the same 8, and exact elsewhere), so that sums of random signs are off by 1.5e-5 of their size: far below a rounding to bf16
-// (up to 2^-8), and more than fp32 results may be off.
+// 2^16 where the two are among the same 8, and exact elsewhere), towards zero: nothing is lost where these are within 2^6 of one another, as products of two e4m3 values have 6
+// bits behind the point, and less than 7 2^-13 of the largest at worst.  Sums of K = 8192 are off by 1.5e-5 (normal numbers, random signs) to 7e-5 (outliers, magnitudes over five decades) of their size, and
+// those of one sign too small by 3e-6 and 1e-4: far below a rounding to bf16 (up to 2^-8), of which 1 in 60 turns out otherwise, and more than fp32 results may be off.
 // fp32 results: elements are turned into bf16 with their scale on the way to the matrix instruction (exactly: 4 bits and 8 of exponent), whose products are
 // exact and whose sums are fp32, at half the rate.  Elements under 2^-126 have fewer bits there.
 // A lane holds row lane & 31 and 32 bytes of K; which 32 of the 64 a half of the wavefront holds does not matter, as both operands are dealt alike and a
