@@ -19,11 +19,12 @@
  *   - "dev" pointers are device (HBM) addresses, "host" pointers are host addresses.
  *   - The library allocates no device memory of its own: als_init() carves everything out of one
  *     caller-owned arena, and the als_k_* entry points work on the caller's buffers only.  What the
- *     HIP runtime keeps for its objects is its own: the events and pinned loss buffer of every worker and,
- *     for models whose steps are so short that launching their kernels takes the host longer than the chip
- *     (workers on three different streams or more), one executable graph per worker.  als_init() captures
- *     those on a stream that it creates and destroys, als_destroy() frees them; a capture that fails
- *     is no error, such a worker's steps are launched kernel by kernel.
+ *     HIP runtime keeps for its objects is its own: the events of every worker, its pinned buffer of losses and
+ *     gradient norms and, for models whose steps are so short that launching their kernels takes the host longer
+ *     than the chip (workers on three different streams or more), one executable graph per worker.  als_init()
+ *     captures those on a stream that it creates and destroys, als_set_grad_clip() does so again where the setting
+ *     changes (the old ones are freed), als_destroy() frees them; a capture that fails is no error, such a worker's
+ *     steps are launched kernel by kernel.
  *     Streams are borrowed hipStream_t handles passed as void*.  Calls on a context refuse a worker's
  *     stream that is being captured (ALS_ERR_HIP, nothing enqueued or changed); the als_k_* entry points
  *     can be captured, als_k_gemm_dw_grouped apart, which waits.

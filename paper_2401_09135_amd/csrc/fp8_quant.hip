@@ -4,10 +4,11 @@
 // both orientations; a thread has 8 rows of 8 columns of it in registers, so that a row's largest magnitude is 16 neighbouring lanes' and the bytes of
 // a thread are 8 in a row of either orientation.  The transposed bytes go through LDS (16 KB) to be written as whole rows of 128.
 // Magnitudes are compared as whole numbers, two bf16 at a time, and the conversion divides by the scale: 3 vector instructions an element in bf16 and both
-// orientations.  Scales are written as single bytes, a tile's rows and columns in one store each (51.5 us otherwise), which meet their neighbours in an L2: every XCD has a run of
+// orientations.  Scales are written as single bytes, a tile's rows and columns in one store each (1.5 us of 51 less), which meet their neighbours in an L2: every XCD has a run of
 // neighbouring tiles.
-// 16384 x 3584 bf16, both orientations: 50 us with a scale a row, 46.4 with one a tile (5.1 TB/s, a copy of that size 5.4); with magnitudes in floating point,
-// products by 1 / scale, tiles dealt to the XCDs in turn and ordinary stores 70 and 55.  Bands of tiles column by column, for the transposed scales, gain 1 us of 56, but with
+// 16384 x 3584 bf16, both orientations: 51 us with a scale a row (4.6 TB/s, a copy of that size 5.4), 48.5 with one a tile; one orientation 35.5; fp32 72 and 69, 56 for one orientation
+// (5.2 TB/s).  With magnitudes in floating point,
+// products by 1 / scale, tiles dealt to the XCDs in turn and ordinary stores bf16 took 70 and 55.  Bands of tiles column by column, for the transposed scales, gain 1 us of 56, but with
 // 4096 columns take 74 instead of 67.
 #include "fp8.h"
 

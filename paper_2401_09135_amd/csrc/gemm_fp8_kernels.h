@@ -113,8 +113,9 @@ __device__ __forceinline__ void fp8_order() { asm volatile("" ::: "memory"); }
 
 // How the kernel's results are written: bit 0: R is added, bit 1: C or R is not aligned for 16 bytes a lane, bit 3: where R is added, parts of 128 x 64 may end outside of the matrix.  Kernels of
 // their own, as one that could do all keeps too few registers for the products; tiles of 128 and 64 ask at run time (EPI_ASK).
-// In us, a kernel for all with R / these: 16384 x 896 x 3584 fp32 105 / 101, 16384 x 3584 x 896 fp32 178 / 168, 14638 x 6376 x 563 fp32 402 / 361 (8 rows of R at once at the edges), bf16
-// 16384 x 896 x 3584 without these kinds 90 / 66.
+// One kernel for all with R takes 4 % longer for 16384 x 896 x 3584 fp32, 6 % for 16384 x 3584 x 896 (now 169 us) and 11 % for 14638 x 6376 x 563 (362 us; 8 rows of R at once at the
+// edges); one for all of bf16 36 % for 16384 x 896 x 3584 with R (66 us).  The kernels of the edges keep 25 to 77 registers in scratch memory, the others with fp32 results 5: R at a
+// ragged edge is what costs most beside its floor (362 us, 224 without R).
 constexpr int EPI_ADD = 1, EPI_ANY = 2, EPI_ASK = 4, EPI_EDGE = 8;
 template <int HOW, int TM, int TN, typename TO>
 __device__ __forceinline__ void fp8_epilogue(const f32x16 (&acc)[TM][TN], char* stg, const Fp8Args& g, TO* C, const float* R, int row0, int col0, int lane) {

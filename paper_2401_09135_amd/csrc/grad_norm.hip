@@ -164,8 +164,8 @@ __device__ __forceinline__ void scale_pieces(const void* in, void* out, int64_t 
 }
 
 // count: partial sums that each workgroup adds itself, in the order of grad_norm_kernel, the first one leaving the norm; 0: the norm is in partial[0].  The coefficient and the
-// products with it are in double: a norm of finite gradients can leave fp32's range, and an output is then what it is there, and rounded once (10^8 elements of
-// fp32 255 us, 253.6 in fp32).
+// products with it are in double: a norm of finite gradients can leave fp32's range, and an output is then what it is there, and rounded once (half a percent of 10^8
+// elements).
 __global__ __launch_bounds__(256) void grad_clip_kernel(GradTable t, float* norm, double max_norm, const double* __restrict__ partial, int count) {
   double root;
   if (count) {

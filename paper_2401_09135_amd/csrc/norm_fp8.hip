@@ -2,9 +2,10 @@
 //
 // Memory bounds both: every tensor is read or written once.  A row stays in the registers of a wavefront (d <= 1024), of 256 threads (d <= 4096) or of 1024; a thread
 // has 2 or 4 runs of 4 consecutive elements of it, so that a load or store of fp32 is 1 KB without gaps for a wavefront, and a block of 128 is 32 neighbouring lanes', whose
-// scale needs no LDS.  The backward pass loads a row while it works on the one before.  16384 x 896, forward (fp32 input, all outputs) 39.4 us, 5.6 TB/s; backward (bf16 dy, all
-// outputs) 46.5 us, 5.05 TB/s with the second launch that adds the gain's gradient.  With runs of 8, loaded behind branches, and no row ahead: 43 and 49.5; 16384 x 1023 backward
-// 57 and 70; 16384 x 512 backward 25.4 and 28.5; 1000 x 16000 backward 83 and 85; with 4 runs where 2 reach 16384 x 512 backward 28, 2000 x 8192 forward 56 instead of 46.
+// scale needs no LDS.  The backward pass loads a row while it works on the one before.  16384 x 896, forward (fp32 input, all outputs) 40.3 us, 5.5 TB/s; backward (bf16 dy, all
+// outputs) 47 us, 5 TB/s with the second launch that adds the gain's gradient; LayerNorm 41 and 48.  16384 x 512 20.4 and 25; 16384 x 1023 52 and 58 to 60; 2000 x 8192 47 and 60
+// (LayerNorm 49 and 67); 1000 x 16000 52 and 68 (57 and 76).  With runs of 8, loaded behind branches, and no row ahead 16384 x 896 takes 9 and 6 % longer, 16384 x 1023 backward 23 %,
+// 16384 x 512 backward 12 %; with 4 runs where 2 reach 16384 x 512 backward 10 %, 2000 x 8192 forward 22 %.
 #include "fp8.h"
 
 #include <type_traits>
@@ -117,7 +118,7 @@ __global__ __launch_bounds__(NT == 64 ? 256 : NT) void norm_fwd_kernel(NormFwdAr
     }
   }
   // Sums of a row in double: what they are off by is the same for the whole row, and turns as many of its 8-bit values as lie that near to a border between two.
-  // 5 of the wavefronts' sums are read at once: all 16 are 32 registers, with which a CU has one workgroup of 1024 threads instead of two (2000 x 8192 39 us instead of 33).
+  // 5 of the wavefronts' sums are read at once: all 16 are 32 registers, with which a CU has one workgroup of 1024 threads instead of two (2000 x 8192 19 % longer).
   double mean = 0.0;
   if (CENTER) {
     double sum = 0.0;
@@ -233,8 +234,8 @@ __global__ __launch_bounds__(NT == 64 ? 256 : NT) void norm_bwd_kernel(NormBwdAr
     RowPart<float, NT, RUNS> add = in;
     if (AHEAD) load(row + stride);
     // The mean in double, as in the forward pass: what it is off by is the same for the whole row, adds up in the gain's gradient, and is in fp32 a rounding times the mean over
-    // the spread (rows of 896 with a mean of 1000 spreads: xh off by 5e-5 in the mean, 1.5e-4 at most).  16384 x 896 takes 40.5 us so and 39.8 in fp32, 2000 x 8192 56.7 and 54, 1000 x
-    // 16000 64 and 61 (LayerNorm, bf16 dy).  The mean is taken off in two parts, halved with the row where the difference could leave fp32's range.
+    // the spread (rows of 896 with a mean of 1000 spreads: xh off by 5e-5 in the mean, 1.5e-4 at most).  That costs 1 to 2 % up to 4096 elements a row and 5 % above.  The mean is
+    // taken off in two parts, halved with the row where the difference could leave fp32's range.
     const double mean = CENTER ? row_sum<NT>(sx, sh_mean) / d : 0.0;
     const float whole = (float)mean, half = fabsf(whole) > 0x1p100f ? 0.5f : 1.0f, off = -whole * half, rest = (float)(mean - (double)whole) * half, rc = half < 1.0f ? r * 2.0f : r;
 #pragma unroll
