@@ -362,9 +362,9 @@ extern "C" int als_k_norm_fwd(const void* x, int dtype, const float* resid, cons
   if (rc) return rc;
   if (q && q->block_rows != 1) return set_error(ALS_ERR_INVALID, "als_k_norm_fwd: q must have block_rows 1");
   if (!(eps >= 0) || eps > 1e30) return set_error(ALS_ERR_INVALID, "als_k_norm_fwd: eps must be finite and >= 0");
+  if (rows == 0) return ALS_OK;   // buffers without elements may be null
   if (!y && !q) return set_error(ALS_ERR_INVALID, "als_k_norm_fwd: no output");
   if (!resid != !total) return set_error(ALS_ERR_INVALID, "als_k_norm_fwd: resid and total are both null or neither");
-  if (rows == 0) return ALS_OK;
   if (!x || !gain || !rstd) return set_error(ALS_ERR_INVALID, "als_k_norm_fwd: null argument");
   if ((uintptr_t)x % (dtype == ALS_DTYPE_BF16 ? 2 : 4) || ((uintptr_t)resid | (uintptr_t)gain | (uintptr_t)total | (uintptr_t)rstd) % 4 || (uintptr_t)y % 2)
     return set_error(ALS_ERR_INVALID, "als_k_norm_fwd: a tensor is not aligned to its type");

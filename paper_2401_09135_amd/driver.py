@@ -15,8 +15,8 @@ def run_async(w: dict, theta0: np.ndarray, make_stream, n_events: int | None = N
     int32 [n,B,S+1] token batches for worker i.  Returns dict like the oracle's run.
     on_group(ctx, index of the group's last event): optional observer called after every applied
     group of sync events (before its workers are given new rounds).
-    grad_clip: norm that the local steps' gradients are clipped to, 0 for no clipping (None: as ctx is set); the
-    norms before clipping are then in the result's grad_norms."""
+    grad_clip: norm that the local steps' gradients are clipped to, 0 for no clipping, and so ctx stays set (None: as ctx
+    is set); where it clips, the norms before clipping are in the result's grad_norms, if losses are collected."""
     import torch
     n_events = w["n_events"] if n_events is None else n_events
     steps, ev_w, ev_t, ev_g = dylu_schedule(w["speeds"], w["H"], w["tau_grace"], n_events)
